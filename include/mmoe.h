@@ -81,7 +81,10 @@ typedef enum {
     MMOE_ERR_MULTIPLE = -8,  /* d_model or d_ff is not a multiple of 256                 */
     MMOE_ERR_LIMIT = -9,     /* E, S or the problem size exceeds the limits above        */
     MMOE_ERR_LAUNCH = -10,   /* the HIP runtime refused a kernel launch                  */
-    MMOE_ERR_STATIC_LIMIT = -11 /* the shape needs more than MMOE_STATIC_WORKSPACE_BYTES     */
+    MMOE_ERR_STATIC_LIMIT = -11, /* the shape needs more than MMOE_STATIC_WORKSPACE_BYTES    */
+    MMOE_ERR_HEAD = -12,     /* a head size, rotated part or number of heads is not supported */
+    MMOE_ERR_STRIDE = -13,   /* a stride is too short or not a multiple of 16 bytes          */
+    MMOE_ERR_FORMAT = -14    /* unknown cache format, rotary layout or scaling, or one that does not go with the type */
 } mmoe_status;
 
 typedef struct {
@@ -358,6 +361,198 @@ int mmoe_assemble_pool(const mmoe_loader_shape *shape, const void *const *mats, 
  */
 int mmoe_validate_inputs(const mmoe_shape *shape, const int32_t *vid, const int32_t *M, void *ws,
                          size_t ws_bytes, void *stream);
+
+/*
+ * ---- The attention half of a served layer -------------------------------------------------------
+ *
+ * What runs in front of the experts for the same batch of tokens of several variants: projections that
+ * the variants share, each with its own low-rank adapter beside them; rotary positions; a paged cache of
+ * keys and values, as they are or in 8 bits; attention of the tokens just added over that cache.  (The
+ * paper calls everything but the experts a variant's non-expert layers, section 3.2.)  The conventions
+ * above hold: device pointers, the caller's stream and workspace, no allocation, no host
+ * synchronisation, negative codes for what the host can check.  Strides are in elements; 0 means dense.
+ * Pointers and strides are multiples of 16 bytes unless a line says otherwise.
+ */
+
+/*
+ * Projection with adapters.
+ *   Y[t,:] = X[t,:] W + scale[a] (X[t,:] A[a]) B[a],  a = aid[t];  without the second term where aid[t]
+ *   is outside [0, n_adapters) (-1 by convention) or n_adapters is 0.
+ * All products accumulate in fp32.  With bf16 storage scale[a] (X A) goes into the second product as two
+ * bf16 parts that together hold 16 bits of it, and Y is rounded once.
+ */
+typedef struct {
+    int32_t T;          /* tokens                                                        */
+    int32_t d_in;       /* inputs K, multiple of 256, up to 65536                        */
+    int32_t d_out;      /* outputs N, multiple of 256, up to 262144                      */
+    int32_t n_adapters; /* adapters, 0..1024                                             */
+    int32_t rank;       /* rank R of the adapters, 1..128 (shorter ones padded with zeros); ignored without adapters */
+    int32_t dtype;      /* mmoe_dtype of X, the weights and Y                            */
+    int64_t ldx, ldy;   /* elements from one token's row to the next; 0: d_in, d_out     */
+} mmoe_project_shape;
+
+/* Host only, pure.  Workspace (bytes) of mmoe_project, never less for fewer tokens; 0 if the shape is invalid. */
+size_t mmoe_project_workspace_bytes(const mmoe_project_shape *shape);
+
+/* Host only, pure.  Elements of the packed adapters: the rank is padded to a multiple of 32 (fp32: 16).  0 if invalid. */
+size_t mmoe_project_packed_rank(const mmoe_project_shape *shape);
+
+/*
+ * One-time packing, when the weights are loaded.  W [K, N], A [n, K, R], B [n, R, N] (in x out) to Wp (K*N
+ * elements), Ap (n*Rp*K), Bp (n*N*Rp), Rp = mmoe_project_packed_rank().  A packed matrix with Q outputs and K
+ * inputs is the sequence [Q/16][K/c][64 lanes] of 16-byte pieces, c = 32 (bf16) or 16 (fp32): piece
+ * 16 g + r holds inputs c k + (c/4) g + [0, c/4) of output 16 q + r, which is what lane 16 g + r of a
+ * matrix instruction holds.  Outputs must not overlap inputs.
+ */
+int mmoe_pack_projection(const mmoe_project_shape *shape, const void *W, void *Wp, void *stream);
+int mmoe_pack_adapters(const mmoe_project_shape *shape, const void *A, const void *B, void *Ap, void *Bp, void *stream);
+
+/*
+ * X [T, d_in] (rows ldx apart), aid [T] int32, scale [n_adapters] fp32, Y [T, d_out] (rows ldy apart) out.  aid, Ap,
+ * Bp and scale may be NULL when n_adapters is 0.  Y must not overlap X.  Results do not depend on the order in which
+ * workgroups run.  Uses `ws`.
+ */
+int mmoe_project(const mmoe_project_shape *shape, const void *X, const int32_t *aid, const void *Wp, const void *Ap,
+                 const void *Bp, const float *scale, void *Y, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Rotary positions.  Pair i of a head, i < rot/2, is (x[i], x[i + rot/2]) (MMOE_ROTARY_HALVES) or (x[2i],
+ * x[2i+1]) (MMOE_ROTARY_NEIGHBOURS) and turns by the angle pos[t] f_i:
+ *   y0 = m (x0 cos - x1 sin),  y1 = m (x0 sin + x1 cos);   with `transpose` the sine's sign is swapped: the
+ *   transposed map, which takes a gradient of y to the gradient of x.
+ * Elements from rot on are copied.  Angles are kept in units of 2^-64 turn, where whole turns overflow: they are
+ * exact to 2^-32 turn at every position.
+ *
+ * f_i = base^(-2i/rot), changed for contexts longer than `original`, the one trained for, by `factor`:
+ *   LINEAR  f_i / factor
+ *   BASE    base * factor^(rot/(rot-2)) takes the place of base
+ *   RAMP    between pair numbers lo = floor(p(32)) >= 0 and hi = ceil(p(1)) <= rot - 1, p(b) = rot ln(original / (2 pi b)) / (2 ln base)
+ *           (the pair that makes b turns in `original` tokens): f_i up to lo, f_i / factor from hi on, a linear
+ *           mixture between; m = 0.1 ln(factor) + 1
+ *   BANDS   with u = original f_i / (2 pi) turns: f_i where u >= 4, f_i / factor where u <= 1, the linear mixture in u between
+ * m = 1 but for RAMP.
+ */
+typedef enum { MMOE_ROTARY_HALVES = 0, MMOE_ROTARY_NEIGHBOURS = 1 } mmoe_rotary_layout;
+typedef enum {
+    MMOE_SCALE_NONE = 0,
+    MMOE_SCALE_LINEAR = 1,
+    MMOE_SCALE_BASE = 2,
+    MMOE_SCALE_RAMP = 3,
+    MMOE_SCALE_BANDS = 4
+} mmoe_rotary_scaling;
+
+typedef struct {
+    int32_t T;         /* tokens                                                  */
+    int32_t heads;     /* heads of a token                                        */
+    int32_t head_dim;  /* D, multiple of 16, up to 512                            */
+    int32_t rot;       /* rotated elements of a head, multiple of 16, up to D     */
+    int32_t layout;    /* mmoe_rotary_layout                                      */
+    int32_t dtype;     /* mmoe_dtype of X and Y                                   */
+    int32_t transpose; /* 0 or 1                                                  */
+    float magnitude;   /* m above                                                 */
+    int64_t x_token, x_head, y_token, y_head; /* strides; 0: heads*D and D        */
+} mmoe_rotary_shape;
+
+/* Host only, pure.  steps [rot/2] (HOST out): f_i / (2 pi) in units of 2^-64, to be copied to the device; *magnitude (HOST
+ * out) the m above. */
+int mmoe_rotary_steps(int32_t rot, double base, int32_t scaling, double factor, int32_t original, uint64_t *steps,
+                      float *magnitude);
+
+/* X, Y [T, heads, D] (Y = X with equal strides: in place; otherwise they must not overlap); pos [T] int32, of either
+ * sign; steps [rot/2] (8-byte aligned).  The arithmetic is fp32; Y is rounded once. */
+int mmoe_rotary(const mmoe_rotary_shape *shape, const void *X, const int32_t *pos, const uint64_t *steps, void *Y, void *stream);
+
+/*
+ * Paged cache of keys and values.  A page holds MMOE_PAGE_TOKENS tokens; place p is row p mod 64 of page p / 64.  A
+ * token's head is kept as it is (MMOE_CACHE_PLAIN) or as D codes of 8 bits with one fp32 scale:
+ *   amax = max |x|;  inv = top / amax (0 where amax is 0);  scale = amax * (1 / top);
+ *   INT8 (top 127): code = x inv rounded to the nearest integer, ties to even;
+ *   FP8  (top 448): code = x inv in e4m3 (no infinities), to nearest, ties to even.
+ * A head with a value that is not finite gets a scale of NaN and codes of zero, and reads back as NaN; one whose
+ * amax is under 2^-100 gets zeros.
+ *
+ * Layout, for what reads pages directly.  K and V of a page and head are 64*D elements each, [n_pages, kv_heads, 64*D];
+ * scales [n_pages, kv_heads, 64] fp32.  A piece is 16 bytes, E elements (8 bf16, 4 fp32, 16 codes).
+ *   K, row r, element d:  ((r/16 * (D/(4E)) + d/(4E)) * 64 + (d mod 4E)/E * 16 + r mod 16) * E + d mod E
+ *   V, row r, element d:  with q = r/16, g = (r mod 16)/4, j = 4q + r mod 4 (0..15):
+ *                         ((d/16 * (16/E) + j/E) * 64 + g * 16 + d mod 16) * E + j mod E
+ * INT8 codes are stored plus 128.
+ */
+#define MMOE_PAGE_TOKENS 64
+typedef enum { MMOE_CACHE_PLAIN = 0, MMOE_CACHE_INT8 = 1, MMOE_CACHE_FP8 = 2 } mmoe_cache_format;
+
+typedef struct {
+    int32_t n_pages;
+    int32_t kv_heads; /* 1..1024                                  */
+    int32_t head_dim; /* D: 64, 128 or 256                        */
+    int32_t dtype;    /* mmoe_dtype of what is appended and read  */
+    int32_t format;   /* mmoe_cache_format                        */
+} mmoe_cache_shape;
+
+typedef struct {      /* DEVICE pointers; the scales are NULL for PLAIN */
+    void *k, *v;
+    float *k_scale, *v_scale;
+} mmoe_cache;
+
+/* Host only, pure.  Bytes of k (and of v); *scale_bytes (may be NULL) those of k_scale (and of v_scale).  0 if invalid. */
+size_t mmoe_cache_bytes(const mmoe_cache_shape *shape, size_t *scale_bytes);
+
+typedef struct {
+    int32_t T;                                   /* tokens to append                                */
+    int64_t k_token, k_head, v_token, v_head;    /* strides of K and V; 0: kv_heads*D and D         */
+} mmoe_cache_rows;
+
+/*
+ * Appends K, V [T, kv_heads, D]: token t to place places[t] (int32; tokens whose place is outside the pages are skipped;
+ * places must differ).  With `rotary` (and pos, steps) the keys are rotated first; what is kept is then what
+ * mmoe_rotary's output, rounded to dtype, would give (its T, heads and strides are ignored, head_dim and dtype have to match).
+ */
+int mmoe_cache_append(const mmoe_cache_shape *shape, const mmoe_cache_rows *rows, const void *K, const void *V,
+                      const int32_t *places, const mmoe_rotary_shape *rotary, const int32_t *pos, const uint64_t *steps,
+                      const mmoe_cache *cache, void *stream);
+
+/* Reads places[r], r < R, back to K, V [R, kv_heads, D] (dense): code * scale in fp32, rounded to dtype.  A place outside the
+ * pages reads as zeros. */
+int mmoe_cache_read(const mmoe_cache_shape *shape, const mmoe_cache *cache, int32_t R, const int32_t *places, void *K, void *V,
+                    void *stream);
+
+/*
+ * Attention of drafted tokens over the cache.  Request b has ctx[b] committed tokens and the n = starts[b+1] - starts[b]
+ * tokens starts[b] .. of Q, whose keys and values are in the cache already, behind the committed ones: token i of the
+ * request is position ctx[b] + i, and position j lives in row j mod 64 of page pages[b, j/64].
+ * Token i sees every committed position and
+ *   with `tree`:  drafted token j < n where bit j mod 64 of tree[starts[b] + i, j/64] is set: the token itself, what it
+ *                 descends from, or whatever else the caller asks for, itself not included if its bit is not;
+ *   without:      drafted tokens j <= i (a chunk of a prompt, or a single token).
+ * Query head h reads key head h / (heads / kv_heads).
+ *   out[t,h] = sum_j softmax_j(scale <Q[t,h], K[j]>) V[j];  lse[t,h] = ln sum_j exp(scale <Q[t,h], K[j]>)
+ * A token that sees nothing gets zeros and an lse of -infinity.  What a token does not see does not reach it, whatever it
+ * holds: rows of a page past the end, infinities, NaN.  Scores, maxima, sums and outputs are fp32.  The probabilities are
+ * rounded for the second product: to bf16 over PLAIN bf16 pages, to fp16 over 8-bit ones, whose codes fp16 holds exactly
+ * (and queries there to fp16, relative to the row's largest; with fp32 nothing is rounded).  8-bit formats need dtype bf16 here.
+ */
+typedef struct {
+    mmoe_cache_shape cache;
+    int32_t T;          /* rows of Q, starts[n_requests]                                          */
+    int32_t n_requests;
+    int32_t heads;      /* query heads, a multiple of kv_heads, up to 64 to a key head            */
+    int32_t max_pages;  /* columns of `pages`; positions from 64*max_pages on are not seen        */
+    int32_t max_drafts; /* no request has more tokens in Q; what goes beyond is not written       */
+    int32_t mask_words; /* 64-bit words of a row of `tree`                                        */
+    int32_t max_keys;   /* hint: the longest ctx + n; 0: 64*max_pages.  Results do not depend on the hints beyond rounding */
+    int64_t sum_keys;   /* hint: the sum of ctx + n; 0: n_requests * max_keys                     */
+    float scale;        /* of the scores                                                          */
+    int64_t q_token, q_head, o_token, o_head; /* strides of Q and out; 0: heads*D and D           */
+} mmoe_attend_shape;
+
+/* Host only, pure.  Workspace (bytes), 0 if the shape is invalid. */
+size_t mmoe_attend_workspace_bytes(const mmoe_attend_shape *shape);
+
+/* Q [T, heads, D], starts [n_requests + 1], ctx [n_requests], tree [T, mask_words] uint64 or NULL, pages [n_requests,
+ * max_pages] int32 (entries outside [0, n_pages) are not seen); out [T, heads, D] dtype, lse [T, heads] fp32 or NULL.  Rows of Q
+ * that belong to no request are left as they are in `out`.  Uses `ws`. */
+int mmoe_attend(const mmoe_attend_shape *shape, const void *Q, const int32_t *starts, const int32_t *ctx, const uint64_t *tree,
+                const int32_t *pages, const mmoe_cache *cache, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

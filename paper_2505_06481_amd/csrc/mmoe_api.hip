@@ -141,6 +141,9 @@ const char* mmoe_strerror(int status)
         case MMOE_ERR_STATIC_LIMIT:
             return "the shape needs more scratch than mmoe_layer_forward_static holds "
                    "(MMOE_STATIC_WORKSPACE_BYTES); use mmoe_layer_forward with a workspace";
+        case MMOE_ERR_HEAD: return "a head size, rotated part or number of heads is not supported";
+        case MMOE_ERR_STRIDE: return "a stride is shorter than what it steps over or not a multiple of 16 bytes";
+        case MMOE_ERR_FORMAT: return "unknown cache format, rotary layout or scaling, or one that does not go with the type";
         default: return "unknown status";
     }
 }

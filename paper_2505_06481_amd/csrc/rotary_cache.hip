@@ -1,0 +1,372 @@
+// Rotary positions, and the paged cache of keys and values: append (with rotation of the keys) and read back.
+//
+// All three are bound by HBM (a few launches' latency for the tokens of one decode step): every element is read and
+// written once, in 16-byte accesses where its neighbours are in the same thread.
+#include <math.h>
+
+#include "attn_internal.h"
+
+namespace mmoe {
+
+// 16 consecutive elements as fp32.
+template <bool F32>
+__device__ __forceinline__ void load8(const char* p, float* x)
+{
+    if constexpr (F32) {
+        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    } else {
+        const u32x4 a = *(const u32x4*)p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(a[i]), x[2 * i + 1] = bf16_hi(a[i]);
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void store8(char* p, const float* x)
+{
+    if constexpr (F32) {
+        *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
+        *(f32x4*)(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+        *(u32x4*)p = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+    }
+}
+
+// A unit is 16 elements of a head: two runs of 8.  Units below rot/16 hold 8 pairs: runs 8u and rot/2 + 8u (halves), or the 16
+// elements from 16u on (neighbours); the units behind them are the elements that are copied.
+struct UnitPlace {
+    int a, b;  // first elements of the runs
+};
+template <bool HALVES>
+__device__ __forceinline__ UnitPlace unit_place(int u, int rot)
+{
+    if (HALVES && u < rot / 16) return {8 * u, rot / 2 + 8 * u};
+    return {16 * u, 16 * u + 8};
+}
+
+// Cosine and sine of pairs 8u .. 8u+7 at a position, times m.  steps: turns per position in units of 2^-64; the product's
+// overflow is whole turns.  The upper 32 bits, as a signed number, are the angle in [-1/2, 1/2) turn.
+__device__ __forceinline__ void turn_of(const uint64_t* __restrict__ steps, int pos, float m, float sign, float* c, float* s)
+{
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint64_t turns = steps[i] * (uint64_t)(int64_t)pos;
+        const float half_turns = (float)(int32_t)(turns >> 32) * 0x1p-31f;
+        float sn, cs;
+        sincospif(half_turns, &sn, &cs);
+        c[i] = cs * m;
+        s[i] = sn * (m * sign);
+    }
+}
+
+template <bool HALVES>
+__device__ __forceinline__ void rotate(float* x, const float* c, const float* s)
+{
+#pragma clang fp contract(off)  // the same bits from every kernel that rotates
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int p = HALVES ? i : 2 * i, q = HALVES ? 8 + i : 2 * i + 1;
+        const float a = x[p], b = x[q];
+        x[p] = __builtin_fmaf(a, c[i], -(b * s[i]));
+        x[q] = __builtin_fmaf(a, s[i], b * c[i]);
+    }
+}
+
+// A wavefront takes a share of the heads of one token.  Lane l holds unit l mod U of head l / U, then of the heads that follow in
+// steps of what the wavefronts of the token cover, so its sines are made once.
+template <bool F32, bool HALVES>
+__global__ __launch_bounds__(256) void rotary_kernel(const char* X, const int32_t* __restrict__ pos, const uint64_t* __restrict__ steps,
+                                                     char* Y, int T, int heads, int D, int rot, int waves, float m, float sign,
+                                                     int64_t xt, int64_t xh, int64_t yt, int64_t yh, bool in_place)
+{
+    constexpr int kEsz = F32 ? 4 : 2;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int t = (int)(wave / waves), part = (int)(wave % waves);
+    if (t >= T) return;
+    const int lane = threadIdx.x & 63, U = D / 16, across = 64 / U;
+    if (lane >= across * U) return;
+    const int u = lane % U;
+    const bool turns = u < rot / 16;
+    if (!turns && in_place) return;
+    float c[8], s[8];
+    if (turns) turn_of(steps + 8 * u, pos[t], m, sign, c, s);
+    const UnitPlace at = unit_place<HALVES>(u, rot);
+    for (int h = part * across + lane / U; h < heads; h += waves * across) {
+        const char* x = X + (t * xt + h * xh) * kEsz;
+        char* y = Y + (t * yt + h * yh) * kEsz;
+        float v[16];
+        load8<F32>(x + at.a * kEsz, v);
+        load8<F32>(x + at.b * kEsz, v + 8);
+        if (turns) rotate<HALVES>(v, c, s);
+        store8<F32>(y + at.a * kEsz, v);
+        store8<F32>(y + at.b * kEsz, v + 8);
+    }
+}
+
+int launch_rotary(const mmoe_rotary_shape& s, const void* X, const int32_t* pos, const uint64_t* steps, void* Y, hipStream_t st)
+{
+    const int across = 64 / (s.head_dim / 16);
+    const int most = (s.heads + across - 1) / across;
+    const int waves = s.T >= 4096 ? 1 : s.T * (int64_t)most <= 8192 ? most : (8192 + s.T - 1) / s.T;
+    const int64_t xh = s.x_head ? s.x_head : s.head_dim, xt = s.x_token ? s.x_token : (int64_t)s.heads * s.head_dim;
+    const int64_t yh = s.y_head ? s.y_head : s.head_dim, yt = s.y_token ? s.y_token : (int64_t)s.heads * s.head_dim;
+    const dim3 grid((unsigned)(((int64_t)s.T * waves + 3) / 4)), block(256);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, st, (const char*)X, pos, steps, (char*)Y, s.T, s.heads, s.head_dim, s.rot, waves,
+                           s.magnitude, s.transpose ? -1.0f : 1.0f, xt, xh, yt, yh, X == Y && xt == yt && xh == yh);
+    };
+    const bool halves = s.layout == MMOE_ROTARY_HALVES;
+    if (s.dtype == MMOE_F32) halves ? go(rotary_kernel<true, true>) : go(rotary_kernel<true, false>);
+    else halves ? go(rotary_kernel<false, true>) : go(rotary_kernel<false, false>);
+    return launch_status();
+}
+
+// ---- cache --------------------------------------------------------------------------------------------
+// What a page holds (the layout is in mmoe.h).  E elements to a piece of 16 bytes.
+template <int FORMAT, bool F32>
+struct Kept {
+    static constexpr bool kPlain = FORMAT == MMOE_CACHE_PLAIN;
+    static constexpr int kBytes = kPlain ? (F32 ? 4 : 2) : 1;  // of an element
+    static constexpr int E = 16 / kBytes;
+    __device__ static int k_at(int r, int d, int D) { return ((((r >> 4) * (D / (4 * E)) + d / (4 * E)) * 64) + (d % (4 * E)) / E * 16 + (r & 15)) * E + d % E; }
+    __device__ static int v_at(int r, int d)
+    {
+        const int j = (r >> 4) * 4 + (r & 3);
+        return (((d >> 4) * (16 / E) + j / E) * 64 + ((r & 15) >> 2) * 16 + (d & 15)) * E + j % E;
+    }
+};
+
+constexpr float kTop[3] = {0.0f, 127.0f, 448.0f};
+constexpr float kLeast = 0x1p-100f;
+
+// Code of one value (bits), and of a code the value.
+template <int FORMAT>
+__device__ __forceinline__ uint32_t code_of(float x)
+{
+    if constexpr (FORMAT == MMOE_CACHE_INT8) return (uint32_t)((int)rintf(x) + 128) & 0xFF;
+    else return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xFF;
+}
+template <int FORMAT>
+__device__ __forceinline__ float value_of(uint32_t code)
+{
+    if constexpr (FORMAT == MMOE_CACHE_INT8) return (float)((int)code - 128);
+    else return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
+}
+
+struct AppendArgs {
+    const char *K, *V;
+    const int32_t* places;
+    const int32_t* pos;
+    const uint64_t* steps;
+    char *k, *v;
+    float *k_scale, *v_scale;
+    int64_t kt, kh, vt, vh;  // strides
+    int T, heads, D, rot;
+    int64_t n_places;
+    float m, sign;
+};
+
+// A workgroup appends 16 tokens of one head: thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8
+// each in one piece; values, whose pieces hold several tokens, through LDS, where four tokens in consecutive places become one store.
+// ROTATE: 0 no, 1 halves, 2 neighbours.
+template <int FORMAT, bool F32, int ROTATE>
+__global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
+{
+    using P = Kept<FORMAT, F32>;
+    constexpr int kEsz = F32 ? 4 : 2, kTok = 16;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int U = g.D / 16, nthreads = 2 * kTok * U, tid = threadIdx.x;
+    char* codes = lds;                                      // [kTok][D] of V
+    float* amax = (float*)(lds + kTok * g.D * P::kBytes);   // [2][kTok][U]
+    __shared__ int place[kTok], run[kTok];
+    const int t0 = blockIdx.x * kTok, h = blockIdx.y;
+    if (tid < kTok) {
+        const int p = t0 + tid < g.T ? g.places[t0 + tid] : -1;
+        place[tid] = p >= 0 && p < g.n_places ? p : -1;
+    }
+    __syncthreads();
+    if (tid < kTok) {  // 4: first of four consecutive places from a multiple of four on; 0: one of the others of such a run; 1: alone
+        const int p = place[tid], lead = tid - (p & 3);
+        bool whole = p >= 0 && lead >= 0 && lead + 3 < kTok;
+        for (int i = 0; i < 4 && whole; ++i) whole = place[lead + i] == (p & ~3) + i;
+        run[tid] = p < 0 ? 0 : !whole ? 1 : (p & 3) == 0 ? 4 : 0;
+    }
+    const int which = tid / (kTok * U), tok = tid / U % kTok, u = tid % U;  // which: 0 keys, 1 values
+    const int t = min(t0 + tok, g.T - 1);
+    const int p = place[tok];
+    const char* src = which ? g.V + (t * g.vt + h * g.vh) * kEsz : g.K + (t * g.kt + h * g.kh) * kEsz;
+    const bool turns = ROTATE && which == 0 && u < g.rot / 16;
+    const UnitPlace at = ROTATE == 1 && which == 0 ? unit_place<true>(u, g.rot) : unit_place<false>(u, g.rot);
+    float x[16];
+    load8<F32>(src + at.a * kEsz, x);
+    load8<F32>(src + at.b * kEsz, x + 8);
+    if (turns) {
+        float c[8], s[8];
+        turn_of(g.steps + 8 * u, g.pos[t], g.m, g.sign, c, s);
+        rotate<ROTATE == 1>(x, c, s);
+        if constexpr (!F32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = bf16_bits_to_f32(f32_to_bf16_bits(x[i]));
+        }
+    }
+    uint32_t code[16];
+    if constexpr (!P::kPlain) {
+        float a = 0.0f;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            a = fmaxf(a, fabsf(x[i]));
+            odd = odd || !(fabsf(x[i]) < INFINITY);
+        }
+        amax[(which * kTok + tok) * U + u] = odd ? INFINITY : a;
+        __syncthreads();
+        a = 0.0f;
+        for (int i = 0; i < U; ++i) a = fmaxf(a, amax[(which * kTok + tok) * U + i]);
+        const bool fine = a < INFINITY && a >= kLeast;
+        const float inv = fine ? kTop[FORMAT] / a : 0.0f;
+        const float scale = a < INFINITY ? (fine ? a * (float)(1.0 / (double)kTop[FORMAT]) : 0.0f) : NAN;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) code[i] = code_of<FORMAT>(fine ? x[i] * inv : 0.0f);
+        if (u == 0 && p >= 0) (which ? g.v_scale : g.k_scale)[((int64_t)(p / kPage) * g.heads + h) * kPage + p % kPage] = scale;
+    }
+    const int64_t block = (int64_t)kPage * g.D;
+    if (which == 0) {
+        if (p >= 0) {
+            char* k = g.k + ((int64_t)(p / kPage) * g.heads + h) * block * P::kBytes;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int d = half ? at.b : at.a;
+                char* dst = k + (int64_t)P::k_at(p % kPage, d, g.D) * P::kBytes;
+                const float* v = x + 8 * half;
+                if constexpr (P::kPlain && F32) {
+                    *(f32x4*)dst = f32x4{v[0], v[1], v[2], v[3]};
+                    *(f32x4*)(k + (int64_t)P::k_at(p % kPage, d + 4, g.D) * 4) = f32x4{v[4], v[5], v[6], v[7]};
+                } else if constexpr (P::kPlain) {
+                    store8<false>(dst, v);
+                } else {
+                    const uint32_t* q = code + 8 * half;
+                    *(u32x2*)dst = u32x2{q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24};
+                }
+            }
+        }
+    } else {
+        char* row = codes + (tok * g.D + 16 * u) * P::kBytes;
+        if constexpr (P::kPlain) {
+            store8<F32>(row, x);
+            store8<F32>(row + 8 * kEsz, x + 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                ((uint32_t*)row)[i] = code[4 * i] | code[4 * i + 1] << 8 | code[4 * i + 2] << 16 | code[4 * i + 3] << 24;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < kTok * g.D; i += nthreads) {
+        const int d = i % g.D, k = i / g.D, n = run[k];
+        if (!n) continue;
+        const int q = place[k];
+        char* dst = g.v + (((int64_t)(q / kPage) * g.heads + h) * block + P::v_at(q % kPage, d)) * P::kBytes;
+        const char* from = codes + (k * g.D + d) * P::kBytes;
+        const int next = g.D * P::kBytes;
+        if constexpr (P::kBytes == 1) {
+            if (n == 4)
+                *(uint32_t*)dst = (uint32_t)(uint8_t)from[0] | (uint32_t)(uint8_t)from[next] << 8 | (uint32_t)(uint8_t)from[2 * next] << 16 |
+                                  (uint32_t)(uint8_t)from[3 * next] << 24;
+            else *dst = *from;
+        } else if constexpr (P::kBytes == 2) {
+            const auto at16 = [&](int j) { return (uint32_t) * (const uint16_t*)(from + j * next); };
+            if (n == 4) *(u32x2*)dst = u32x2{at16(0) | at16(1) << 16, at16(2) | at16(3) << 16};
+            else *(uint16_t*)dst = *(const uint16_t*)from;
+        } else {
+            const auto at32 = [&](int j) { return *(const uint32_t*)(from + j * next); };
+            if (n == 4) *(u32x4*)dst = u32x4{at32(0), at32(1), at32(2), at32(3)};
+            else *(uint32_t*)dst = *(const uint32_t*)from;
+        }
+    }
+}
+
+template <int FORMAT, bool F32>
+static void append(const mmoe_rotary_shape* rotary, const AppendArgs& g, hipStream_t st)
+{
+    const int U = g.D / 16, kept = Kept<FORMAT, F32>::kBytes;
+    const dim3 grid((g.T + 15) / 16, g.heads), block(2 * 16 * U);
+    const size_t lds = (size_t)16 * g.D * kept + 2 * 16 * U * sizeof(float);
+    if (!rotary) hipLaunchKernelGGL((append_kernel<FORMAT, F32, 0>), grid, block, lds, st, g);
+    else if (rotary->layout == MMOE_ROTARY_HALVES) hipLaunchKernelGGL((append_kernel<FORMAT, F32, 1>), grid, block, lds, st, g);
+    else hipLaunchKernelGGL((append_kernel<FORMAT, F32, 2>), grid, block, lds, st, g);
+}
+
+int launch_cache_append(const mmoe_cache_shape& s, const mmoe_cache_rows& rows, const void* K, const void* V, const int32_t* places,
+                        const mmoe_rotary_shape* rotary, const int32_t* pos, const uint64_t* steps, const mmoe_cache& cache,
+                        hipStream_t st)
+{
+    const int64_t hd = s.head_dim, td = (int64_t)s.kv_heads * s.head_dim;
+    AppendArgs g = {(const char*)K, (const char*)V, places, pos, steps, (char*)cache.k, (char*)cache.v, cache.k_scale, cache.v_scale,
+                    rows.k_token ? rows.k_token : td, rows.k_head ? rows.k_head : hd, rows.v_token ? rows.v_token : td,
+                    rows.v_head ? rows.v_head : hd, rows.T, s.kv_heads, s.head_dim, rotary ? rotary->rot : 0,
+                    (int64_t)s.n_pages * kPage, rotary ? rotary->magnitude : 1.0f, rotary && rotary->transpose ? -1.0f : 1.0f};
+    const bool f32 = s.dtype == MMOE_F32;
+    switch (s.format) {
+        case MMOE_CACHE_PLAIN: f32 ? append<MMOE_CACHE_PLAIN, true>(rotary, g, st) : append<MMOE_CACHE_PLAIN, false>(rotary, g, st); break;
+        case MMOE_CACHE_INT8: f32 ? append<MMOE_CACHE_INT8, true>(rotary, g, st) : append<MMOE_CACHE_INT8, false>(rotary, g, st); break;
+        default: f32 ? append<MMOE_CACHE_FP8, true>(rotary, g, st) : append<MMOE_CACHE_FP8, false>(rotary, g, st); break;
+    }
+    return launch_status();
+}
+
+// A thread reads 16 elements of a row's keys or values back: adjacent threads have adjacent rows, whose pieces are neighbours.
+template <int FORMAT, bool F32>
+__global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, const char* __restrict__ v, const float* __restrict__ ks,
+                                                   const float* __restrict__ vs, const int32_t* __restrict__ places,
+                                                   char* __restrict__ K, char* __restrict__ V, int R, int heads, int D, int64_t n_places)
+{
+    using P = Kept<FORMAT, F32>;
+    constexpr int kEsz = F32 ? 4 : 2;
+    const int U = D / 16, h = blockIdx.y, which = blockIdx.z;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = id / (16 * U) * 16 + id % 16;  // 16 rows, unit by unit
+    const int u = (int)(id / 16 % U);
+    if (r >= R) return;
+    const int p = places[r];
+    float x[16];
+    if (p < 0 || p >= n_places) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    } else {
+        const int64_t ph = (int64_t)(p / kPage) * heads + h;
+        const char* base = (which ? v : k) + ph * kPage * D * P::kBytes;
+        float scale = 1.0f;
+        if constexpr (!P::kPlain) scale = (which ? vs : ks)[ph * kPage + p % kPage];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const char* at = base + (int64_t)(which ? P::v_at(p % kPage, 16 * u + i) : P::k_at(p % kPage, 16 * u + i, D)) * P::kBytes;
+            if constexpr (P::kPlain && F32) x[i] = *(const float*)at;
+            else if constexpr (P::kPlain) x[i] = bf16_bits_to_f32(*(const uint16_t*)at);
+            else x[i] = value_of<FORMAT>(*(const uint8_t*)at) * scale;
+        }
+    }
+    char* out = (which ? V : K) + ((r * heads + h) * D + 16 * u) * kEsz;
+    store8<F32>(out, x);
+    store8<F32>(out + 8 * kEsz, x + 8);
+}
+
+int launch_cache_read(const mmoe_cache_shape& s, const mmoe_cache& c, int R, const int32_t* places, void* K, void* V, hipStream_t st)
+{
+    const int U = s.head_dim / 16;
+    const dim3 grid((unsigned)(((int64_t)(R + 15) / 16 * 16 * U + 255) / 256), s.kv_heads, 2), block(256);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, st, (const char*)c.k, (const char*)c.v, c.k_scale, c.v_scale, places, (char*)K, (char*)V,
+                           R, s.kv_heads, s.head_dim, (int64_t)s.n_pages * kPage);
+    };
+    const bool f32 = s.dtype == MMOE_F32;
+    switch (s.format) {
+        case MMOE_CACHE_PLAIN: f32 ? go(read_kernel<MMOE_CACHE_PLAIN, true>) : go(read_kernel<MMOE_CACHE_PLAIN, false>); break;
+        case MMOE_CACHE_INT8: f32 ? go(read_kernel<MMOE_CACHE_INT8, true>) : go(read_kernel<MMOE_CACHE_INT8, false>); break;
+        default: f32 ? go(read_kernel<MMOE_CACHE_FP8, true>) : go(read_kernel<MMOE_CACHE_FP8, false>); break;
+    }
+    return launch_status();
+}
+
+}  // namespace mmoe

@@ -25,12 +25,18 @@ _ACTS = {"relu": RELU, "swiglu": SWIGLU, "gelu": GELU}
 _GATES = {"selected": GATE_SELECTED, "all": GATE_ALL}
 _TORCH_DT = {F32: torch.float32, BF16: torch.bfloat16}
 
+# the attention half: their signatures are set where they are bound (attention.py)
+ATTENTION_EXPORTS = [
+    "mmoe_project_workspace_bytes", "mmoe_project_packed_rank", "mmoe_pack_projection", "mmoe_pack_adapters", "mmoe_project",
+    "mmoe_rotary_steps", "mmoe_rotary", "mmoe_cache_bytes", "mmoe_cache_append", "mmoe_cache_read",
+    "mmoe_attend_workspace_bytes", "mmoe_attend",
+]
 EXPORTS = [
     "mmoe_workspace_bytes", "mmoe_strerror", "mmoe_pack_weights", "mmoe_route", "mmoe_remap_permute",
     "mmoe_expert_ffn", "mmoe_combine", "mmoe_layer_forward", "mmoe_layer_forward_events",
     "mmoe_layer_forward_static", "mmoe_layer_forward_paged", "mmoe_loader_workspace_bytes", "mmoe_expert_distance", "mmoe_build_expert_map",
     "mmoe_assemble_pool", "mmoe_validate_inputs", "mmoe_probe_ceilings", "mmoe_expert_plan",
-]
+] + ATTENTION_EXPORTS
 
 
 class MmoeError(RuntimeError):
@@ -103,7 +109,7 @@ def lib():
         L.mmoe_expert_plan.argtypes = [sp, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]
         L.mmoe_probe_ceilings.argtypes = [vp, sz, ctypes.POINTER(ctypes.c_float), vp]
         for n in EXPORTS[2:]:
-            if n != "mmoe_loader_workspace_bytes":
+            if n != "mmoe_loader_workspace_bytes" and n not in ATTENTION_EXPORTS:
                 getattr(L, n).restype = i
         _lib = L
     return _lib

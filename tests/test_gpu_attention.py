@@ -1,0 +1,661 @@
+"""The attention half on the GPU, through the binding, against the plain 64-bit definitions in oracle/attention.py.
+
+Tolerances.  Inputs are of unit size; u = 2^-8 is the largest relative error of rounding to bf16 (8 significant bits: 1 + 2^-8 lies
+half way between its neighbours 1 and 1 + 2^-7), 2^-24 that of fp32.
+  project, bf16: the base product is exact to fp32; the adapter's U is held in 16 bits, the result is rounded once:
+    2^-8 |ref| + 2^-6 rms(adapter part) + 1e-4 rms.
+  fp32: sums of K terms in chains of K/4 or less: 4 sqrt(K) 2^-24 rms per element at most 5 sigma, taken as 2e-5 rms.
+  rotary: three roundings and sines of 2 ulp: 8 * 2^-24 of the pair's size, plus u |y| in bf16.
+  cache: 8-bit codes are defined in fp32 and compared exactly, but for rotated keys (one code off at a tie).
+  attend: probabilities rounded to bf16 (u) or fp16 (2^-11), averaged: |err| <= u max|v| + u |out| in bf16; fp32 1e-5 max|v|; lse
+    1e-5 (1 + |lse|), scores being sums of D <= 256 terms in fp32.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def at():
+    from paper_2505_06481_amd import attention
+    return attention
+
+
+@pytest.fixture(scope="module")
+def ref():
+    from oracle import attention
+    return attention
+
+
+def rand(gen, *shape, dtype="f32", scale=1.0):
+    return (torch.randn(*shape, generator=gen) * scale).to(DT[dtype])
+
+
+def gen_of(*key):
+    return torch.Generator().manual_seed(hash(key) % (1 << 31))
+
+
+def close(got, want, tol, what=""):
+    got = got.detach().double().cpu()
+    assert got.shape == want.shape, f"{what}: {got.shape} {want.shape}"
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf], want[inf]) and torch.equal(torch.isinf(got), inf), f"{what}: infinities"
+    fine = torch.isfinite(want)
+    err = torch.where(fine, (got - want).abs(), torch.zeros_like(want))
+    tol = tol.expand_as(want) if torch.is_tensor(tol) else torch.full_like(want, tol)
+    worst = (err - tol)[fine]
+    assert worst.numel() == 0 or worst.max() <= 0, f"{what}: off by {err[fine].max():.3g}, {int((worst > 0).sum())} of {want.numel()} outside"
+
+
+def rms(x):
+    return float(x.double().square().mean().sqrt()) if x.numel() else 0.0
+
+
+# ---------------------------------------------------------------- projection with adapters
+def run_project(at, ref, T, K, N, n, R, dtype, mix="random", ldx=0, ldy=0, ws_for=None, seed=0):
+    g = gen_of(1, T, K, N, n, R, seed)
+    X, W = rand(g, T, K, dtype=dtype), rand(g, K, N, dtype=dtype, scale=K ** -0.5)
+    A, B = rand(g, n, K, R, dtype=dtype, scale=K ** -0.5), rand(g, n, R, N, dtype=dtype, scale=R ** -0.5)
+    scale = torch.rand(n, generator=g) + 0.5
+    aid = {"random": torch.randint(-1, n, (T,), generator=g), "blocks": torch.arange(T) * n // T, "turns": torch.arange(T) % n,
+           "none": torch.full((T,), -1), "one": torch.full((T,), n - 1), "wild": torch.randint(-5, n + 5, (T,), generator=g)}[mix]
+    aid = aid.to(torch.int32)
+    shape = at.make_project_shape(T, K, N, n, R, dtype, ldx=ldx, ldy=ldy)
+    Xd = X.cuda()
+    if ldx:
+        Xd = torch.full((T, ldx), math.nan, dtype=DT[dtype], device="cuda")
+        Xd[:, :K] = X.cuda()
+        Xd = Xd[:, :K]
+    Y = None
+    if ldy:
+        wide = torch.full((T, ldy), 7.0, dtype=DT[dtype], device="cuda")
+        Y = wide[:, :N]
+    ws = at.project_workspace(ws_for or shape)
+    ws.fill_(0xFF)  # NaN in every type
+    Wp = at.pack_projection(shape, W.cuda())
+    Ap, Bp = at.pack_adapters(shape, A.cuda(), B.cuda())
+    Y = at.project(shape, Xd, aid.cuda(), Wp, Ap, Bp, scale.cuda(), ws, Y=Y)
+    again = at.project(shape, Xd, aid.cuda(), Wp, Ap, Bp, scale.cuda(), ws)
+    torch.cuda.synchronize()
+    assert torch.equal(Y, again), "two runs differ"
+    if ldy:
+        assert bool((wide[:, N:] == 7.0).all()), "wrote between the rows"
+    want = ref.project(X, aid, W, A, B, scale)
+    part = want - X.double() @ W.double()
+    if dtype == "bf16":
+        tol = 2.0 ** -8 * want.abs() + 2.0 ** -6 * rms(part) + 1e-4 * rms(want)
+    else:
+        tol = torch.full_like(want, 2e-5 * rms(want))
+    close(Y, want, tol, f"project {T} {K} {N} {n} {R} {dtype} {mix}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 33, 64, 65, 130, 257])
+def test_project_lengths(at, ref, T, dtype):
+    run_project(at, ref, T, 512, 768, 3, 16, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R", [1, 7, 16, 31, 33, 64, 128])
+def test_project_ranks(at, ref, R, dtype):
+    run_project(at, ref, 40, 256, 512, 4, R, dtype)
+    run_project(at, ref, 300, 256, 256, 4, R, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mix", ["blocks", "turns", "none", "one", "wild"])
+@pytest.mark.parametrize("T,n", [(5, 1), (64, 40), (400, 2), (700, 70)])
+def test_project_mixes(at, ref, T, n, mix, dtype):
+    run_project(at, ref, T, 256, 512, n, 8, dtype, mix=mix)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 70, 513])
+def test_project_strides(at, ref, T, dtype):
+    run_project(at, ref, T, 256, 512, 3, 12, dtype, ldx=256 + 8, ldy=512 + 24)
+
+
+@pytest.mark.parametrize("T,K,N,n,R,dtype", [(1, 4096, 256, 2, 16, "bf16"), (64, 4096, 1024, 48, 16, "bf16"), (520, 2304, 1280, 3, 32, "bf16"),
+                                             (1030, 1024, 2048, 5, 20, "bf16"), (2100, 256, 4352, 2, 64, "bf16"), (9, 4096, 512, 4, 8, "f32"),
+                                             (350, 1024, 768, 2, 16, "f32")])
+def test_project_sizes(at, ref, T, K, N, n, R, dtype):
+    run_project(at, ref, T, K, N, n, R, dtype)
+
+
+def test_project_many_adapters_and_a_larger_workspace(at, ref):
+    run_project(at, ref, 90, 256, 256, 1024, 4, "bf16", mix="random")
+    big = at.make_project_shape(4096, 256, 512, 9, 16, "bf16")
+    for T in (1, 100, 1000):
+        assert at.project_workspace_bytes(at.make_project_shape(T, 256, 512, 9, 16, "bf16")) <= at.project_workspace_bytes(big)
+        run_project(at, ref, T, 256, 512, 9, 16, "bf16", ws_for=big)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 20, 200])
+def test_project_without_adapters(at, ref, T, dtype):
+    g = gen_of(2, T)
+    X, W = rand(g, T, 512, dtype=dtype), rand(g, 512, 256, dtype=dtype, scale=512 ** -0.5)
+    shape = at.make_project_shape(T, 512, 256, 0, 0, dtype)
+    Y = at.project(shape, X.cuda(), None, at.pack_projection(shape, W.cuda()), None, None, None, at.project_workspace(shape))
+    want = X.double() @ W.double()
+    close(Y, want, (2.0 ** -8 if dtype == "bf16" else 0.0) * want.abs() + 2e-5 * rms(want))
+
+
+def test_project_keeps_other_tokens_apart(at):
+    """A token with infinities, and an adapter with NaN, reach nobody else."""
+    for T in (24, 300):
+        g = gen_of(3, T)
+        X, W = rand(g, T, 256, dtype="bf16"), rand(g, 256, 512, dtype="bf16", scale=1 / 16)
+        A, B = rand(g, 3, 256, 8, dtype="bf16", scale=1 / 16), rand(g, 3, 8, 512, dtype="bf16")
+        A[1] = math.nan
+        X[5] = math.inf
+        aid = torch.arange(T, dtype=torch.int32) % 3
+        shape = at.make_project_shape(T, 256, 512, 3, 8, "bf16")
+        args = [at.pack_projection(shape, W.cuda()), *at.pack_adapters(shape, A.cuda(), B.cuda()), torch.ones(3, device="cuda")]
+        Y = at.project(shape, X.cuda(), aid.cuda(), *args, at.project_workspace(shape)).cpu()
+        bad = torch.isnan(Y.float()).any(1) | torch.isinf(Y.float()).any(1)
+        assert torch.equal(bad, (aid == 1) | (torch.arange(T) == 5))
+
+
+def test_project_packed_layout(at):
+    for dtype, c in (("bf16", 32), ("f32", 16)):
+        K, N, n, R = 256, 512, 2, 12
+        g = gen_of(4)
+        W, A, B = rand(g, K, N, dtype=dtype), rand(g, n, K, R, dtype=dtype), rand(g, n, R, N, dtype=dtype)
+        shape = at.make_project_shape(4, K, N, n, R, dtype)
+        Wp = at.pack_projection(shape, W.cuda()).cpu()
+        Ap, Bp = (x.cpu() for x in at.pack_adapters(shape, A.cuda(), B.cuda()))
+        rp = {"bf16": 32, "f32": 16}[dtype]
+
+        def unpacked(p, S, Q, I):  # -> [S, I, Q]
+            return p.view(S, Q // 16, I // c, 4, 16, c // 4).permute(0, 2, 3, 5, 1, 4).reshape(S, I, Q)
+        assert torch.equal(unpacked(Wp, 1, N, K)[0], W)
+        a, b = unpacked(Ap, n, rp, K), unpacked(Bp, n, N, rp)
+        assert torch.equal(a[:, :, :R], A) and not a[:, :, R:].any()
+        assert torch.equal(b[:, :R], B) and not b[:, R:].any()
+
+
+# ---------------------------------------------------------------- rotary positions
+def run_rotary(at, ref, T, H, D, rot, layout, dtype, scaling="none", transpose=False, behind=0, in_place=False, heads_first=False, start=0):
+    g = gen_of(5, T, H, D, rot)
+    X = rand(g, H, T, D, dtype=dtype).transpose(0, 1) if heads_first else rand(g, T, H + behind, D, dtype=dtype)[:, :H]
+    pos = (torch.arange(T) * 37 % max(T, 1) + start).to(torch.int32)
+    steps, magnitude = at.rotary_steps(rot, 10000.0, scaling, 8.0, 4096)
+    freqs, m = ref.frequencies(rot, 10000.0, scaling, 8.0, 4096)
+    assert abs(m - magnitude) < 1e-6
+    shape = at.make_rotary_shape(T, H, D, rot, layout, dtype, magnitude, transpose)
+    Xd = torch.empty_strided(X.size(), X.stride(), dtype=X.dtype, device="cuda").copy_(X) if not behind else \
+        torch.cat([X, torch.full((T, behind, D), 5.0, dtype=X.dtype)], 1).cuda()[:, :H]
+    Y = at.rotary(shape, Xd, pos.cuda(), steps, Y=Xd if in_place else None)
+    if in_place:
+        assert Y.data_ptr() == Xd.data_ptr()
+        if behind:
+            assert bool((Xd._base[:, H:] == 5.0).all())
+    want = ref.rotary(X, pos, freqs, m, rot, layout, transpose)
+    # angles: 2^-25 turn, and the double's own product in the definition
+    tol = (2.0 ** -8 if dtype == "bf16" else 0.0) * want.abs() + (1e-6 + 1e-15 * abs(start)) * m * 2 * X.double().abs().amax()
+    close(Y, want, tol, f"rotary {T} {H} {D} {rot} {layout} {dtype} {scaling}")
+    if not transpose and rot < D:
+        assert torch.equal(Y[..., rot:].cpu(), X[..., rot:])
+
+
+@pytest.mark.parametrize("layout", ["halves", "neighbours"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,D,rot", [(1, 1, 16, 16), (1, 32, 128, 128), (3, 5, 64, 16), (7, 12, 80, 32), (2, 40, 96, 96), (65, 3, 256, 128),
+                                       (5, 2, 512, 512), (4, 9, 128, 64)])
+def test_rotary(at, ref, T, H, D, rot, layout, dtype):
+    run_rotary(at, ref, T, H, D, rot, layout, dtype)
+    run_rotary(at, ref, T, H, D, rot, layout, dtype, transpose=True, behind=3, in_place=True, scaling="ramp")
+
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "base", "ramp", "bands"])
+@pytest.mark.parametrize("start", [0, 4000, 131072, 1000003, -50])
+def test_rotary_scalings_and_positions(at, ref, scaling, start):
+    run_rotary(at, ref, 9, 2, 128, 128, "halves", "f32", scaling=scaling, start=start)
+    run_rotary(at, ref, 9, 2, 64, 32, "neighbours", "f32", scaling=scaling, start=start)
+
+
+@pytest.mark.parametrize("T,H", [(300, 40), (5000, 3), (9000, 1)])
+def test_rotary_many_tokens(at, T, H):
+    """Against the kernel's own single-token calls, which the other tests check."""
+    g = gen_of(6, T)
+    X = rand(g, T, H, 64, dtype="bf16").cuda()
+    pos = torch.randint(0, 100000, (T,), generator=g).to(torch.int32).cuda()
+    steps, m = at.rotary_steps(64)
+    Y = at.rotary(at.make_rotary_shape(T, H, 64, 64, "halves", "bf16", m), X, pos, steps)
+    one = at.make_rotary_shape(1, H, 64, 64, "halves", "bf16", m)
+    for t in (0, 1, T // 2, T - 1):
+        assert torch.equal(Y[t:t + 1], at.rotary(one, X[t:t + 1], pos[t:t + 1].clone(), steps))
+
+
+def test_rotary_heads_outermost(at, ref):
+    run_rotary(at, ref, 6, 3, 64, 64, "halves", "bf16", heads_first=True)
+
+
+def test_rotary_transpose_is_the_gradient(at):
+    """<g, R(x + e d) - R(x - e d)> / 2e = <R^T g, d>: the map is linear, so differences are exact but for rounding."""
+    g = gen_of(7)
+    T, H, D = 5, 3, 64
+    x, d, gy = (rand(g, T, H, D).cuda() for _ in range(3))
+    pos = torch.randint(0, 5000, (T,), generator=g).to(torch.int32).cuda()
+    for layout in ("halves", "neighbours"):
+        steps, m = at.rotary_steps(32, 10000.0, "ramp", 4.0, 2048)
+        f = at.make_rotary_shape(T, H, D, 32, layout, "f32", m)
+        b = at.make_rotary_shape(T, H, D, 32, layout, "f32", m, transpose=True)
+        diff = (at.rotary(f, x + d, pos, steps).double() - at.rotary(f, x - d, pos, steps).double()) / 2
+        left, right = (gy.double() * diff).sum(), (at.rotary(b, gy, pos, steps).double() * d.double()).sum()
+        assert abs(float(left - right)) < 1e-5 * math.sqrt(T * H * D)
+
+
+# ---------------------------------------------------------------- cache
+def heads_of(g, T, H, D, dtype):
+    x = rand(g, T, H, D, dtype=dtype)
+    x[..., ::7] *= 9.0
+    if T > 2:
+        x[1, 0] = 0.0
+        x[2, H - 1] *= 1e-30
+    return x
+
+
+@pytest.mark.parametrize("format", ["plain", "int8", "fp8"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,D,start", [(1, 1, 64, 5), (3, 2, 128, 62), (16, 8, 128, 0), (17, 3, 64, 1), (70, 2, 256, 30), (200, 4, 128, 3),
+                                         (260, 1, 64, 64)])
+def test_cache_round_trip(at, ref, T, H, D, start, dtype, format):
+    g = gen_of(8, T, H, D)
+    pages = (start + T + 63) // 64 + 2
+    K, V = heads_of(g, T, H, D, dtype), heads_of(g, T, H, D, dtype)
+    order = torch.randperm(pages, generator=g)
+    at_ = torch.arange(start, start + T)
+    places = (order[at_ // 64] * 64 + at_ % 64).to(torch.int32)
+    shape = at.make_cache_shape(pages, H, D, dtype, format)
+    cache = at.alloc_cache(shape)
+    for t in cache:
+        if t is not None:
+            t.view(torch.uint8).fill_(0xFF)
+    wide = torch.cat([K, V, K[:, :1]], 1).cuda()  # views into a wider row
+    at.cache_append(shape, wide[:, :H], wide[:, H:2 * H], places.cuda(), cache)
+    k, v = at.cache_read(shape, cache, places.cuda())
+    for got, x in ((k, K), (v, V)):
+        want = ref.kept(x, format)
+        if format == "plain":
+            assert torch.equal(got.cpu(), x)
+        else:  # codes are exact; one product in fp32, rounded to dtype
+            close(got, want, want.abs() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) + 1e-38, f"{T} {H} {D} {dtype} {format}")
+    # any order, twice the same, and outside
+    pick = torch.randint(0, T, (37,), generator=g)
+    some = places[pick].clone()
+    some[3], some[4] = -1, pages * 64
+    k2, v2 = at.cache_read(shape, cache, some.cuda())
+    for got, x in ((k2, k), (v2, v)):
+        want = x.cpu()[pick]
+        want[3:5] = 0
+        assert torch.equal(got.cpu(), want)
+
+
+def test_cache_layout(at):
+    """Pages hold what the header says, where it says."""
+    H, D, T = 2, 128, 64
+    g = gen_of(9)
+    for dtype, format in (("bf16", "plain"), ("f32", "plain"), ("bf16", "int8")):
+        K, V = rand(g, T, H, D, dtype=dtype), rand(g, T, H, D, dtype=dtype)
+        shape = at.make_cache_shape(3, H, D, dtype, format)
+        cache = at.alloc_cache(shape)
+        at.cache_append(shape, K.cuda(), V.cuda(), (64 + torch.arange(T)).to(torch.int32).cuda(), cache)
+        E = {"bf16": 8, "f32": 4}[dtype] if format == "plain" else 16
+        r, d = torch.meshgrid(torch.arange(64), torch.arange(D), indexing="ij")
+        ka = ((r // 16 * (D // (4 * E)) + d // (4 * E)) * 64 + d % (4 * E) // E * 16 + r % 16) * E + d % E
+        j = r // 16 * 4 + r % 4
+        va = ((d // 16 * (16 // E) + j // E) * 64 + r % 16 // 4 * 16 + d % 16) * E + j % E
+        for x, buf, at_, scales in ((K, cache.k, ka, cache.k_scale), (V, cache.v, va, cache.v_scale)):
+            assert torch.equal(at_.flatten().sort()[0], torch.arange(64 * D))
+            page = buf.cpu().view(DT[dtype] if format == "plain" else torch.uint8).view(3, H, 64 * D)[1]
+            for h in range(H):
+                got = page[h][at_.flatten()].view(64, D)
+                if format == "plain":
+                    assert torch.equal(got, x[:, h])
+                else:
+                    want = (got.float() - 128) * scales.cpu().view(3, H, 64)[1, h][:, None]
+                    step = x[:, h].float().abs().amax(-1, keepdim=True) / 127
+                    assert bool(((want - x[:, h].float()).abs() <= 0.5001 * step).all())
+
+
+@pytest.mark.parametrize("format", ["int8", "fp8"])
+def test_cache_values_that_are_not_finite(at, format):
+    g = gen_of(10)
+    K, V = rand(g, 9, 2, 64, dtype="bf16"), rand(g, 9, 2, 64, dtype="bf16")
+    K[1, 0, 5], V[4, 1, 63], V[7, 0, 0] = math.nan, math.inf, -math.inf
+    shape = at.make_cache_shape(2, 2, 64, "bf16", format)
+    cache = at.alloc_cache(shape)
+    places = torch.arange(20, 29).to(torch.int32).cuda()
+    at.cache_append(shape, K.cuda(), V.cuda(), places, cache)
+    k, v = (x.cpu().float() for x in at.cache_read(shape, cache, places))
+    for got, x in ((k, K), (v, V)):
+        bad = ~torch.isfinite(x.float()).all(-1)
+        assert torch.equal(torch.isnan(got).all(-1), bad) and bool(torch.isfinite(got[~bad]).all())
+
+
+@pytest.mark.parametrize("format", ["plain", "int8", "fp8"])
+@pytest.mark.parametrize("layout,rot", [("halves", 128), ("halves", 64), ("neighbours", 128), ("neighbours", 32)])
+def test_cache_rotates_keys(at, layout, rot, format):
+    """The same bytes as rotating first and appending then."""
+    g = gen_of(11)
+    T, H, D = 37, 3, 128
+    K, V = rand(g, T, H, D, dtype="bf16").cuda(), rand(g, T, H, D, dtype="bf16").cuda()
+    pos = torch.randint(0, 200000, (T,), generator=g).to(torch.int32).cuda()
+    steps, m = at.rotary_steps(rot, 10000.0, "ramp", 8.0, 4096)
+    turn = at.make_rotary_shape(T, H, D, rot, layout, "bf16", m)
+    shape = at.make_cache_shape(2, H, D, "bf16", format)
+    places = (torch.randperm(128, generator=g)[:T]).to(torch.int32).cuda()
+    a, b = at.alloc_cache(shape), at.alloc_cache(shape)
+    for c in (a, b):
+        for t in c:
+            if t is not None:
+                t.zero_()
+    at.cache_append(shape, K, V, places, a, rotary=(turn, steps, pos))
+    at.cache_append(shape, at.rotary(turn, K, pos, steps), V, places, b)
+    for x, y in zip(a, b):
+        assert x is y or torch.equal(x, y)
+
+
+def test_cache_skips_places_outside(at):
+    shape = at.make_cache_shape(1, 1, 64, "bf16", "plain")
+    cache = at.alloc_cache(shape)
+    cache.k.zero_(), cache.v.zero_()
+    x = torch.ones(5, 1, 64, dtype=torch.bfloat16, device="cuda")
+    at.cache_append(shape, x, x, torch.tensor([-1, 64, 3, 1 << 30, -(1 << 30)], dtype=torch.int32, device="cuda"), cache)
+    k, v = at.cache_read(shape, cache, torch.arange(64, dtype=torch.int32, device="cuda"))
+    for t in (k, v):
+        assert t.float().sum() == 64 and t[3].float().sum() == 64
+
+
+# ---------------------------------------------------------------- attention
+class Paged:
+    """Requests with contexts and drafts on random pages, filled with values that are not to be read elsewhere."""
+
+    def __init__(self, at, ref, g, ctx, drafts, H, Hkv, D, dtype, format, spare=2, K=None, V=None):
+        self.ctx, self.drafts = ctx, drafts
+        lengths = [c + n for c, n in zip(ctx, drafts)]
+        own = [(n + 63) // 64 for n in lengths]
+        self.wide = max(own) + 1
+        self.n_pages = sum(own) + spare
+        order = torch.randperm(self.n_pages, generator=g).tolist()
+        self.pages = torch.full((len(ctx), self.wide), -7, dtype=torch.int32)
+        self.shape = at.make_cache_shape(self.n_pages, Hkv, D, dtype, format)
+        self.cache = at.alloc_cache(self.shape)
+        for t in self.cache:
+            if t is not None:
+                t.view(torch.uint8).fill_(0xFF)  # NaN in bf16, fp32 and e4m3
+        self.keys, self.values, i = [], [], 0
+        for b, n in enumerate(lengths):
+            for p in range(own[b]):
+                self.pages[b, p] = order[i]
+                i += 1
+            k = rand(g, n, Hkv, D, dtype=dtype) if K is None else K[b]
+            v = rand(g, n, Hkv, D, dtype=dtype) if V is None else V[b]
+            at_ = torch.arange(n)
+            places = (self.pages[b][at_ // 64] * 64 + at_ % 64).to(torch.int32)
+            at.cache_append(self.shape, k.cuda(), v.cuda(), places.cuda(), self.cache)
+            self.keys.append(ref.kept(k, format))
+            self.values.append(ref.kept(v, format))
+        self.starts = torch.tensor([0] + list(np.cumsum(drafts)), dtype=torch.int32)
+        self.T = int(self.starts[-1])
+        self.Q = rand(g, self.T, H, D, dtype=dtype)
+
+
+def trees(g, drafts, words=None):
+    most = max(max(drafts), 1)
+    words = words or (most + 63) // 64
+    out = torch.zeros(sum(drafts), words, dtype=torch.int64)
+    t = 0
+    for n in drafts:
+        seen = []
+        for i in range(n):
+            parent = int(torch.randint(max(-1, i - 6), i, (1,), generator=g)) if i else -1
+            seen.append((seen[parent] if parent >= 0 else 0) | 1 << i)
+            for w in range(words):
+                x = seen[i] >> 64 * w & (1 << 64) - 1
+                out[t, w] = x - (1 << 64) if x >> 63 else x
+            t += 1
+    return out
+
+
+def attend_tol(dtype, format, values, want):
+    big = max(float(v.abs().nan_to_num(0, 0, 0).max()) if v.numel() else 0.0 for v in values)
+    if dtype == "f32":
+        return 1e-5 * big + 0.0 * want.nan_to_num(0, 0, 0)
+    return 2.0 ** -8 * big + 2.0 ** -8 * want.abs().nan_to_num(0, 0, 0)
+
+
+def check_attend(at, ref, p, H, D, dtype, format, tree, scale=None, **hints):
+    scale = D ** -0.5 if scale is None else scale
+    shape = at.make_attend_shape(p.shape, p.T, len(p.ctx), H, p.wide, max(max(p.drafts), 1), scale,
+                                 mask_words=None if tree is None else tree.shape[1], **hints)
+    ws = at.attend_workspace(shape)
+    ws.fill_(0xFF)
+    out, lse = at.attend(shape, p.Q.cuda(), p.starts.cuda(), torch.tensor(p.ctx, dtype=torch.int32).cuda(),
+                         None if tree is None else tree.cuda(), p.pages.cuda(), p.cache, ws)
+    torch.cuda.synchronize()
+    want, want_lse = ref.attend(p.Q, p.starts, p.ctx, tree, p.keys, p.values, scale)
+    what = f"attend ctx={p.ctx} drafts={p.drafts} H={H} D={D} {dtype} {format} {hints}"
+    close(lse, want_lse, 1e-5 * (1 + want_lse.abs().nan_to_num(0, 0, 0)), what + " lse")
+    close(out, want, attend_tol(dtype, format, p.values, want), what)
+    return out, lse
+
+
+KINDS = [("bf16", "plain"), ("bf16", "int8"), ("bf16", "fp8"), ("f32", "plain")]
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("G", [1, 4, 7])
+def test_attend_single_tokens(at, ref, G, D, dtype, format):
+    ctx = [0, 1, 14, 15, 16, 63, 64, 65, 127, 300]
+    p = Paged(at, ref, gen_of(12, G, D), ctx, [1] * len(ctx), 2 * G, 2, D, dtype, format)
+    check_attend(at, ref, p, 2 * G, D, dtype, format, None)
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("drafts", [[3, 1, 7], [16, 9, 12], [40, 64, 33], [0, 5, 0]])
+def test_attend_trees(at, ref, drafts, D, dtype, format):
+    g = gen_of(13, D, len(drafts), drafts[0])
+    p = Paged(at, ref, g, [0, 61, 200], drafts, 4, 2, D, dtype, format)
+    check_attend(at, ref, p, 4, D, dtype, format, trees(g, drafts))
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("H,Hkv", [(4, 1), (3, 3), (16, 2)])
+def test_attend_chunks(at, ref, H, Hkv, D, dtype, format):
+    g = gen_of(14, H, D)
+    p = Paged(at, ref, g, [0, 37, 64], [70, 33, 129], H, Hkv, D, dtype, format)
+    check_attend(at, ref, p, H, D, dtype, format, None)
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+def test_attend_wide_trees(at, ref, dtype, format):
+    """More drafted tokens than a word of the mask has bits; more words than the drafts need."""
+    g = gen_of(15)
+    drafts = [130, 65]
+    p = Paged(at, ref, g, [33, 90], drafts, 4, 2, 64, dtype, format)
+    check_attend(at, ref, p, 4, 64, dtype, format, trees(g, drafts, words=4))
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+@pytest.mark.parametrize("drafts", [[1, 1, 1], [5, 2, 4], [40, 20, 33]])
+def test_attend_long_contexts_are_split(at, ref, drafts, dtype, format):
+    """Splits of the keys, joined; hints that are right, missing, or too small."""
+    g = gen_of(16, drafts[0])
+    D, H = 64, 4
+    p = Paged(at, ref, g, [3000, 17, 1100], drafts, H, 2, D, dtype, format)
+    tree = trees(g, drafts)
+    a, _ = check_attend(at, ref, p, H, D, dtype, format, tree, max_keys=3050, sum_keys=4300)
+    b, _ = check_attend(at, ref, p, H, D, dtype, format, tree, max_keys=3050, sum_keys=4300)
+    assert torch.equal(a, b), "two runs differ"
+    check_attend(at, ref, p, H, D, dtype, format, tree)
+    check_attend(at, ref, p, H, D, dtype, format, tree, max_keys=64, sum_keys=1)
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+def test_attend_rows_that_see_nothing(at, ref, dtype, format):
+    """An empty mask over an empty context; a mask without the token itself; requests without drafts."""
+    g = gen_of(17)
+    drafts = [4, 0, 3]
+    p = Paged(at, ref, g, [0, 0, 70], drafts, 4, 2, 64, dtype, format)
+    tree = torch.zeros(7, 1, dtype=torch.int64)
+    tree[1, 0], tree[2, 0], tree[5, 0] = 1, 0b1001, 0b100
+    out, lse = check_attend(at, ref, p, 4, 64, dtype, format, tree)
+    assert not out[0].any() and bool((lse[0] == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts", [6, 40])
+def test_attend_what_is_not_seen_does_not_count(at, ref, dtype, drafts):
+    """Infinities and NaN in keys and values of drafted tokens reach the tokens that see them, and no others."""
+    g = gen_of(18, drafts)
+    ctx = 75
+    K, V = rand(g, ctx + drafts, 2, 64, dtype=dtype), rand(g, ctx + drafts, 2, 64, dtype=dtype)
+    V[ctx + 1, 0, 3], V[ctx + 1, 1, 9], V[ctx + 2, 0, 50], V[ctx + 4, 1, 7], K[ctx + 3, 0, 0] = math.inf, math.nan, -math.inf, math.inf, math.nan
+    p = Paged(at, ref, g, [ctx], [drafts], 4, 2, 64, dtype, "plain", K=[K], V=[V])
+    tree = torch.zeros(drafts, 1, dtype=torch.int64)
+    for i in range(drafts):
+        tree[i, 0] = 1 << i | (1 << 1 if i == 5 else 0)
+    check_attend(at, ref, p, 4, 64, dtype, "plain", tree)
+
+
+@pytest.mark.parametrize("format", ["int8", "fp8"])
+def test_attend_rows_that_are_not_finite_in_8_bits(at, ref, format):
+    g = gen_of(19)
+    K, V = rand(g, 80, 2, 64, dtype="bf16"), rand(g, 80, 2, 64, dtype="bf16")
+    V[75, 0, 3], K[76, 1, 0] = math.inf, math.nan
+    p = Paged(at, ref, g, [72], [8], 4, 2, 64, "bf16", format, K=[K], V=[V])
+    tree = torch.tensor([[1 << i] for i in range(8)], dtype=torch.int64)
+    check_attend(at, ref, p, 4, 64, "bf16", format, tree)
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
+def test_attend_large_and_small_scores(at, ref, dtype, format):
+    """Scores far beyond what an exponential holds, a running maximum that rises at the end, value scales that differ by 2^40."""
+    g = gen_of(20)
+    n = 700
+    K, V = rand(g, n, 1, 64, dtype=dtype), rand(g, n, 1, 64, dtype=dtype)
+    K *= torch.linspace(0.1, 30.0, n)[:, None, None].to(K.dtype)
+    V[:350] *= 2.0 ** -20
+    V[600:] *= 2.0 ** 20
+    p = Paged(at, ref, g, [n - 3], [3], 4, 1, 64, dtype, format, K=[K], V=[V])
+    check_attend(at, ref, p, 4, 64, dtype, format, None, scale=1.0)
+    check_attend(at, ref, p, 4, 64, dtype, format, None, scale=1e-3)
+    check_attend(at, ref, p, 4, 64, dtype, format, None, scale=-0.5)
+
+
+def test_attend_strides_and_pages_outside(at, ref):
+    """Queries inside wider rows, outputs with heads outermost, a page number outside the cache (its tokens are not seen)."""
+    g = gen_of(21)
+    H, D = 4, 64
+    p = Paged(at, ref, g, [130, 10], [2, 3], H, 2, D, "bf16", "plain")
+    shape = at.make_attend_shape(p.shape, p.T, 2, H, p.wide, 3, D ** -0.5)
+    ws = at.attend_workspace(shape)
+    Q = torch.full((p.T, H + 5, D), math.nan, dtype=torch.bfloat16, device="cuda")
+    Q[:, 2:2 + H] = p.Q.cuda()
+    out = torch.zeros(H, p.T, D, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    ctx = torch.tensor(p.ctx, dtype=torch.int32).cuda()
+    at.attend(shape, Q[:, 2:2 + H], p.starts.cuda(), ctx, None, p.pages.cuda(), p.cache, ws, out=out)
+    want, _ = ref.attend(p.Q, p.starts, p.ctx, None, p.keys, p.values, D ** -0.5)
+    close(out, want, attend_tol("bf16", "plain", p.values, want))
+    pages = p.pages.clone()
+    pages[0, 1] = p.n_pages + 3
+    got, _ = at.attend(shape, p.Q.cuda(), p.starts.cuda(), ctx, None, pages.cuda(), p.cache, ws)
+    keep = [j for j in range(132) if j // 64 != 1]
+    G = 2
+    for t in range(2):
+        seen = [j for j in keep if j <= 130 + t]
+        for h in range(H):
+            K, V = p.keys[0][seen, h // G], p.values[0][seen, h // G]
+            o = torch.softmax(K @ p.Q[t, h].double() * D ** -0.5, 0) @ V
+            close(got[t, h], o, attend_tol("bf16", "plain", p.values, o))
+
+
+def test_attend_context_longer_than_the_table(at, ref):
+    g = gen_of(22)
+    p = Paged(at, ref, g, [150], [2], 2, 1, 64, "bf16", "plain")
+    shape = at.make_attend_shape(p.shape, 2, 1, 2, 2, 2, 0.125)  # two pages of three
+    out, _ = at.attend(shape, p.Q.cuda(), p.starts.cuda(), torch.tensor([150], dtype=torch.int32).cuda(), None,
+                       p.pages[:, :2].contiguous().cuda(), p.cache, at.attend_workspace(shape))
+    want, _ = ref.attend(p.Q, p.starts, p.ctx, None, p.keys, p.values, 0.125, limit=128)
+    close(out, want, attend_tol("bf16", "plain", p.values, want))
+
+
+def test_half_runs_on_another_stream(at, ref):
+    g = gen_of(23)
+    p = Paged(at, ref, g, [200, 90], [3, 3], 4, 2, 64, "bf16", "int8")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        check_attend(at, ref, p, 4, 64, "bf16", "int8", None)
+        run_project(at, ref, 40, 256, 256, 3, 8, "bf16")
+    side.synchronize()
+
+
+def test_half_replays_in_a_graph(at):
+    """One step's launches, recorded once and replayed on new inputs, with eager work between the replays."""
+    g = gen_of(24)
+    T, d, H, Hkv, D = 4, 512, 4, 2, 64
+    W = rand(g, d, (H + 2 * Hkv) * D, dtype="bf16", scale=d ** -0.5).cuda()
+    A, B = rand(g, 2, d, 8, dtype="bf16", scale=d ** -0.5).cuda(), rand(g, 2, 8, W.shape[1], dtype="bf16").cuda()
+    ps = at.make_project_shape(T, d, W.shape[1], 2, 8, "bf16")
+    Wp, (Ap, Bp), scale = at.pack_projection(ps, W), at.pack_adapters(ps, A, B), torch.ones(2, device="cuda")
+    cs = at.make_cache_shape(40, Hkv, D, "bf16", "int8")
+    cache = at.alloc_cache(cs)
+    steps, m = at.rotary_steps(D)
+    turn = at.make_rotary_shape(T, H, D, D, "halves", "bf16", m)
+    sh = at.make_attend_shape(cs, T, T, H, 10, 1, D ** -0.5)
+    ws, wsp = at.attend_workspace(sh), at.project_workspace(ps)
+    old = rand(g, 40 * 64, Hkv, D, dtype="bf16").cuda()
+    at.cache_append(cs, old, old, torch.arange(40 * 64, dtype=torch.int32, device="cuda"), cache)
+    pages = torch.arange(40, dtype=torch.int32, device="cuda").view(T, 10)
+    starts = torch.arange(T + 1, dtype=torch.int32, device="cuda")
+    X, aid = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    ctx, places = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    Y = torch.empty(T, W.shape[1], dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda"), torch.empty(T, H, device="cuda")
+
+    def step():
+        at.project(ps, X, aid, Wp, Ap, Bp, scale, wsp, Y=Y)
+        rows = Y.view(T, H + 2 * Hkv, D)
+        at.rotary(turn, rows[:, :H], ctx, steps, Y=rows[:, :H])
+        at.cache_append(cs, rows[:, H:H + Hkv], rows[:, H + Hkv:], places, cache, rotary=(turn, steps, ctx))
+        at.attend(sh, rows[:, :H], starts, ctx, None, pages, cache, ws, out=out, lse=lse)
+
+    def inputs(i):
+        gg = gen_of(25, i)
+        X.copy_(rand(gg, T, d, dtype="bf16"))
+        aid.copy_(torch.randint(-1, 2, (T,), generator=gg))
+        c = torch.randint(0, 600, (T,), generator=gg)
+        ctx.copy_(c)
+        places.copy_((torch.arange(T) * 10 + c // 64) * 64 + c % 64)
+
+    inputs(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(1, 5):
+        inputs(i)
+        step()
+        want = [x.clone() for x in (Y, out, lse)]
+        torch.cuda.synchronize()
+        for x in (Y, out, lse):
+            x.fill_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, w in zip((Y, out, lse), want):
+            assert torch.equal(x, w)
