@@ -388,7 +388,7 @@ typedef struct {
     int32_t n_adapters; /* adapters, 0..1024                                             */
     int32_t rank;       /* rank R of the adapters, 1..128 (shorter ones padded with zeros); ignored without adapters */
     int32_t dtype;      /* mmoe_dtype of X, the weights and Y                            */
-    int64_t ldx, ldy;   /* elements from one token's row to the next; 0: d_in, d_out     */
+    int64_t ldx, ldy;   /* elements from one token's row to the next, up to 2^20; 0: d_in, d_out */
 } mmoe_project_shape;
 
 /* Host only, pure.  Workspace (bytes) of mmoe_project, never less for fewer tokens; 0 if the shape is invalid. */

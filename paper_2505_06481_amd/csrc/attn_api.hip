@@ -29,7 +29,7 @@ int check_project(const mmoe_project_shape* s)
     if (s->d_in % 256 || s->d_out % 256) return MMOE_ERR_MULTIPLE;
     if (s->n_adapters && s->rank <= 0) return MMOE_ERR_DIM;
     if (s->d_in > 65536 || s->d_out > 262144 || s->n_adapters > kMaxAdapters || (s->n_adapters && s->rank > kMaxRank) ||
-        s->T > (1 << 24))
+        s->T > (1 << 24) || (int64_t)s->T * s->d_out >= (int64_t)1 << 40 || s->ldx > kMaxRow || s->ldy > kMaxRow)
         return MMOE_ERR_LIMIT;
     if (bad_stride(s->ldx, s->d_in, s->dtype) || bad_stride(s->ldy, s->d_out, s->dtype)) return MMOE_ERR_STRIDE;
     return MMOE_OK;
@@ -152,7 +152,7 @@ int mmoe_project(const mmoe_project_shape* shape, const void* X, const int32_t* 
     if (int rc = check_project(shape)) return rc;
     if (!X || !Wp || !Y) return MMOE_ERR_NULL;
     if (shape->n_adapters && (!aid || !Ap || !Bp || !scale)) return MMOE_ERR_NULL;
-    const size_t need = project_ws_bytes(*shape);
+    const size_t need = project_need(*shape);
     if (need && (!ws || ws_bytes < need)) return MMOE_ERR_WORKSPACE;
     if (misaligned(X, 16) || misaligned(Wp, 16) || misaligned(Y, 16) || misaligned(Ap, 16) || misaligned(Bp, 16) ||
         misaligned(aid, 4) || misaligned(scale, 4) || misaligned(ws, 256))

@@ -1,6 +1,8 @@
 // Internal declarations of the attention half: projections with adapters, rotary positions, paged cache, attention.
 #pragma once
 
+#include <utility>
+
 #include "mmoe_internal.h"
 
 namespace mmoe {
@@ -11,6 +13,19 @@ typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 constexpr int kPage = MMOE_PAGE_TOKENS;
 constexpr int kMaxAdapters = 1024;
 constexpr int kMaxRank = 128;
+constexpr int64_t kMaxRow = (int64_t)1 << 20;  // row strides of a projection: a tile's rows are addressed with 32 bits
+
+// f(0) .. f(N - 1) with the numbers as constants: register arrays are indexed statically whatever the loop's size.
+template <typename F, int... I>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F&& f)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f)
+{
+    each(std::make_integer_sequence<int, N>{}, f);
+}
 
 // Matrix products on 16-byte operand pieces.  Lane 16 g + r of a wavefront holds, of row r of the operand, the
 // 16 bytes of group g: 8 bf16 of the 32 k of v_mfma_f32_16x16x32_bf16, or 4 fp32 of 16 k, which four
@@ -46,6 +61,7 @@ inline int padded_rank(const mmoe_project_shape& s)
     const int q = s.dtype == MMOE_BF16 ? 32 : 16;
     return (s.rank + q - 1) / q * q;
 }
+size_t project_need(const mmoe_project_shape& s);
 size_t project_ws_bytes(const mmoe_project_shape& s);
 int launch_pack_pieces(const void* in, void* out, int S, int K, int N, int Kp, int Np, int dtype, hipStream_t st);
 int launch_project(const mmoe_project_shape& s, const void* X, const int32_t* aid, const void* Wp, const void* Ap,
