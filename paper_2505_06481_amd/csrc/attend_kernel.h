@@ -1,0 +1,615 @@
+// The attention kernel's template: one translation unit for each kind of page (attend_*.hip).
+//
+// out[t,h] = sum_j softmax_j(scale <Q[t,h], K[j]>) V[j], in one pass over the keys with a reference m for the exponents and the
+// sum l: O holds sum 2^(s_j - m) V_j, and where a step's largest score exceeds m by more than kSlack, m becomes that score and O and
+// l are scaled (everything in base 2: the scores carry log2 e).
+//
+// A column is a (token, query head) pair of one request and key head: all that read the same keys.  A wavefront holds 16 NC
+// columns.  Keys are the row operand of the first product, so a lane has four consecutive keys of a column per tile of 16, which
+// is, with the order in which pages keep values, its part of the column operand of the second: probabilities go
+// from one product to the other inside a lane, and keys and values from memory straight into operand registers, 1 KB an
+// instruction, no LDS and no barrier in the loop.  Queries of more than 16 columns stand in LDS in operand order.
+#pragma once
+#include <math.h>
+
+#include "attn_internal.h"
+
+namespace mmoe {
+
+enum { kBf16 = 0, kInt8 = 1, kFp8 = 2, kF32 = 3 };  // what pages hold
+
+// How a call is shared out: 16-column tiles to a wavefront, whether the wavefronts of a workgroup take different columns or
+// different keys, and splits of the keys.
+struct Shares {
+    int nc, groups, chunk, nsplit;
+    bool cols;
+};
+
+struct AttendArgs {
+    const char* Q;
+    const int32_t *starts, *ctx;
+    const uint64_t* tree;
+    const int32_t* pages;
+    const char *k, *v;
+    const float *k_scale, *v_scale;
+    char* out;
+    float* lse;
+    float* part_o;   // [nsplit][T * heads][D]
+    float* part_ml;  // [nsplit][T * heads][2]
+    int64_t qt, qh, ot, oh;
+    int T, B, heads, kv_heads, G, max_pages, max_drafts, mask_words, n_pages;
+    int groups, nsplit, chunk;  // column groups; splits of the keys, pages of each
+    float scale;
+};
+
+template <int KIND>
+__device__ __forceinline__ f32x4 mma_kind(u32x4 a, u32x4 b, f32x4 c)
+{
+    if constexpr (KIND == kF32) return mma<true>(a, b, c);
+    else if constexpr (KIND == kBf16) return mma<false>(a, b, c);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Four codes as fp16.  Int8: 0x6400 | (code + 128) is 1024 + 128 + code; fp8 has an instruction.
+template <int KIND>
+__device__ __forceinline__ u32x2 widen(uint32_t x)
+{
+    if constexpr (KIND == kInt8) {
+        const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+        const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04010400u)) - bias;
+        const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u)) - bias;
+        return u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+    } else {
+        return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true))};
+    }
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const f16x2 h = {(_Float16)lo, (_Float16)hi};
+    return __builtin_bit_cast(uint32_t, h);
+}
+
+__device__ __forceinline__ float max_groups(float x)  // over the four lane groups
+{
+    x = fmaxf(x, lane_xor<16>(x));
+    return fmaxf(x, lane_xor<32>(x));
+}
+__device__ __forceinline__ float sum_groups(float x)
+{
+    x += lane_xor<16>(x);
+    return x + lane_xor<32>(x);
+}
+
+__device__ __forceinline__ void in_agprs(f32x4& x) { asm volatile("" : "+a"(x)); }
+
+// 2^x; -infinity gives 0.
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kSlack = 8.0f;  // probabilities are up to 2^8: most steps then leave O and l as they are
+constexpr int kLiftBits = 7;    // fp16 ones are lifted by 2^7 (to 2^15 at most), which keeps small ones out of the subnormal range
+
+template <int D, int KIND, int NC>
+struct AttendPlan {
+    static constexpr int kBytes = KIND == kF32 ? 4 : KIND == kBf16 ? 2 : 1;
+    static constexpr int E = 16 / kBytes;
+    static constexpr bool kCodes = KIND == kInt8 || KIND == kFp8;
+    // tiles of 16 keys to a step: 16 KB of keys and values for heads of 128
+    static constexpr int KT = kCodes ? 4 : D * kBytes <= 128 ? 4 : D * kBytes <= 256 || KIND == kBf16 ? 2 : 1;
+    static constexpr int NKS = D / (4 * E);            // pieces of a key row that a lane holds
+    static constexpr int NV = KT * 4 / E == 0 ? 1 : KT * 4 / E;  // value pieces to 16 elements of a step
+    static constexpr int QS = KIND == kF32 ? D / 16 : D / 32;    // query pieces
+    static constexpr int DT = D / 16;
+    static constexpr bool kLdsQ = NC > 1;
+};
+
+// Waves to a SIMD: two where the accumulators and the operands in flight leave half of the registers.
+template <int D, int KIND, int NC>
+constexpr int attend_waves() { return NC == 1 && D <= 128 ? 2 : 1; }
+
+template <int D, int KIND, int NC, bool COLS>
+__global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_kernel(AttendArgs g)
+{
+    using L = AttendPlan<D, KIND, NC>;
+    constexpr int KT = L::KT, NKS = L::NKS, NV = L::NV, QS = L::QS, DT = L::DT, E = L::E, kSteps = 4 / KT;
+    constexpr int NP = KT * 4 / (KIND == kF32 ? 4 : 8);  // operand pieces of the probabilities
+    constexpr bool kCodes = L::kCodes;
+    constexpr int kEsz = KIND == kF32 ? 4 : 2;  // of Q and out
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // column groups of the same keys on one XCD (workgroup id mod 8)
+    int id = blockIdx.x / 8;
+    const int cg = id % g.groups;
+    id = id / g.groups * 8 + blockIdx.x % 8;
+    const int h = id % g.kv_heads;
+    id /= g.kv_heads;
+    const int b = id % g.B, split = id / g.B;
+    if (split >= g.nsplit) return;
+    const int start = g.starts[b], n = min(min(g.starts[b + 1], g.T) - start, g.max_drafts), ctx = g.ctx[b];
+    const int C = n * g.G;
+    constexpr int kWide = COLS ? 64 * NC : 16 * NC;
+    if (start < 0 || cg * kWide >= C || ctx < 0) return;  // uniform
+    const int total = (int)min((int64_t)ctx + n, (int64_t)g.max_pages * kPage);
+    const int all_pages = (total + kPage - 1) / kPage;
+    const int active = min(g.nsplit, max(1, (all_pages + g.chunk - 1) / g.chunk));
+    if (split >= active) return;
+    const int col0 = cg * kWide + (COLS ? wave * 16 * NC : 0);
+
+    // what the last column of these sees at most
+    const int last_token = min(C - 1, cg * kWide + kWide - 1) / g.G;
+    const int limit = g.tree ? total : (int)min((int64_t)total, (int64_t)ctx + last_token + 1);
+    const int step0 = split * g.chunk * kSteps;
+    const int step1 = min(split == active - 1 ? all_pages * kSteps : (split + 1) * g.chunk * kSteps, (limit + 16 * KT - 1) / (16 * KT));
+
+    constexpr int64_t kBlock = (int64_t)kPage * D * L::kBytes;
+    const int32_t* table = g.pages + (int64_t)b * g.max_pages;
+    // Page and head of a step.  A page number outside the cache is page 0 with `hole` set: its keys are not seen.
+    auto page_of = [&](int step) { return __builtin_amdgcn_readfirstlane(table[step / kSteps]); };
+    auto block_of = [&](int page) { return (int64_t)((unsigned)page < (unsigned)g.n_pages ? page : 0) * g.kv_heads + h; };
+    u32x4 kf[KT][NKS], vf[DT][NV];
+    f32x4 ks[KT], vs[KT];
+    auto load_k = [&](int64_t block, int step) {
+        const char* src = g.k + block * kBlock + (step % kSteps) * (KT * NKS * 1024) + lane * 16;
+        each<KT * NKS>([&](auto x) {
+            constexpr int i = decltype(x)::value;
+            kf[i / NKS][i % NKS] = *(const u32x4*)(src + i * 1024);
+        });
+        if constexpr (kCodes)
+            each<KT>([&](auto x) { ks[decltype(x)::value] = *(const f32x4*)(g.k_scale + block * kPage + lg * 4 + decltype(x)::value * 16); });
+    };
+    auto load_v = [&](int64_t block, int step, auto dtc) {
+        constexpr int dt = decltype(dtc)::value;
+        const char* src = g.v + block * kBlock + (step % kSteps) * (NV * 1024) + lane * 16;
+        each<NV>([&](auto x) { vf[dt][decltype(x)::value] = *(const u32x4*)(src + (dt * (16 / E) + decltype(x)::value) * 1024); });
+    };
+    auto load_vs = [&](int64_t block) {
+        if constexpr (kCodes)
+            each<KT>([&](auto x) { vs[decltype(x)::value] = *(const f32x4*)(g.v_scale + block * kPage + lg * 4 + decltype(x)::value * 16); });
+    };
+    constexpr int kStride = COLS ? 1 : 4;
+    int step = step0 + (COLS ? 0 : wave);
+    const bool works = step < step1 && (!COLS || col0 < C);  // uniform over the wavefront
+    int page = 0;
+    if (works) {
+        page = page_of(step);
+        const int64_t block = block_of(page);
+        load_k(block, step);
+        load_vs(block);
+        each<DT>([&](auto dt) { load_v(block, step, dt); });
+    }
+
+    // ---- queries ----
+    constexpr int kQWaves = COLS ? 4 : 1;  // wavefronts with the same columns share them
+    constexpr int kQBytes = L::kLdsQ ? kQWaves * NC * QS * 1024 : 16;
+    constexpr int kRow = 36, kSumBytes = COLS ? 16 : 4 * 16 * NC * kRow * 4;
+    __shared__ __attribute__((aligned(16))) char lds[kQBytes > kSumBytes ? kQBytes : kSumBytes];  // queries, and at the end the join's sums
+    char* const lds_q = lds + (COLS ? wave * NC * QS * 1024 : 0) + lane * 16;
+    u32x4 q_reg[L::kLdsQ ? 1 : QS];
+    float mult[NC];  // of the scores, in base 2; positive
+    int token[NC];   // of the request; n where the column is none
+    each<NC>([&](auto ctc) {
+        constexpr int ct = decltype(ctc)::value;
+        const int c = col0 + ct * 16 + lr;
+        const bool there = c < C && g.scale != 0.0f;
+        token[ct] = c < C ? c / g.G : n;
+        const char* src = g.Q + ((int64_t)(start + (there ? c / g.G : 0)) * g.qt + (int64_t)(h * g.G + (there ? c % g.G : 0)) * g.qh) * kEsz;
+        mult[ct] = g.scale != 0.0f ? fabsf(g.scale) * 1.44269504088896340736f : 1.0f;
+        const uint32_t sign = g.scale < 0.0f ? (KIND == kF32 ? 0x80000000u : 0x80008000u) : 0u;
+        u32x4 q[QS];
+        each<QS>([&](auto x) {
+            constexpr int i = decltype(x)::value;
+            // codes: two instructions of 32 share a piece of 16 codes
+            const int d = kCodes ? (i >> 1) * 64 + lg * 16 + (i & 1) * 8 : i * (KIND == kF32 ? 16 : 32) + lg * (KIND == kF32 ? 4 : 8);
+            q[i] = there ? *(const u32x4*)(src + d * kEsz) ^ sign : u32x4{0, 0, 0, 0};
+        });
+        if constexpr (kCodes) {  // to fp16, by a power of two that puts the largest at 2^12
+            float a = 0.0f;
+            each<QS * 4>([&](auto x) {
+                const uint32_t w = q[decltype(x)::value / 4][decltype(x)::value % 4];
+                a = fmaxf(a, fmaxf(fabsf(bf16_lo(w)), fabsf(bf16_hi(w))));
+            });
+            a = max_groups(a);
+            const int e = a > 0.0f && a < INFINITY ? min(100, 12 - (int)((__float_as_uint(a) >> 23) - 127)) : 0;
+            const float up = ldexpf(1.0f, e);
+            mult[ct] *= ldexpf(1.0f, -e);
+            each<QS * 4>([&](auto x) {
+                constexpr int i = decltype(x)::value / 4, w = decltype(x)::value % 4;
+                q[i][w] = pack_f16(bf16_lo(q[i][w]) * up, bf16_hi(q[i][w]) * up);
+            });
+        }
+        each<QS>([&](auto x) {
+            constexpr int i = decltype(x)::value;
+            if constexpr (!L::kLdsQ) q_reg[i] = q[i];
+            else if (COLS || wave == ct % 4) *(u32x4*)(lds_q + (ct * QS + i) * 1024) = q[i];
+        });
+    });
+    if constexpr (L::kLdsQ) __syncthreads();
+    auto query = [&](int ct, int i) -> u32x4 {
+        if constexpr (L::kLdsQ) return *(const u32x4*)(lds_q + (ct * QS + i) * 1024);
+        else return q_reg[i];
+    };
+
+    f32x4 o[NC][DT];
+    float m[NC], l[NC];
+    each<NC>([&](auto ct) {
+        m[decltype(ct)::value] = -INFINITY;
+        l[decltype(ct)::value] = 0.0f;  // this lane's keys only, until the end
+        each<DT>([&](auto dt) { o[decltype(ct)::value][decltype(dt)::value] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
+    });
+    int lift = -126;  // o holds 2^(kLiftBits - lift) times its value (codes): lift is the largest exponent of a value scale so far
+
+    // Accumulators are read by vector instructions in rare branches only: they stay in AGPRs around them.
+    auto pin = [&](int ct) {
+        if constexpr (attend_waves<D, KIND, NC>() == 1)
+            each<DT>([&](auto dt) { in_agprs(o[ct][decltype(dt)::value]); });
+    };
+    auto fragments = [&](const u32x4& x, u32x4& lo, u32x4& hi) {  // 16 codes as two operands
+        const u32x2 a = widen<KIND>(x[0]), c = widen<KIND>(x[1]), d = widen<KIND>(x[2]), e = widen<KIND>(x[3]);
+        lo = u32x4{a[0], a[1], c[0], c[1]};
+        hi = u32x4{d[0], d[1], e[0], e[1]};
+    };
+
+    while (works && step < step1) {
+        const int next = step + kStride;
+        const bool more = next < step1;
+        const int next_page = more ? page_of(next) : 0;
+        const int64_t next_block = block_of(next_page);
+        const bool hole = (unsigned)page >= (unsigned)g.n_pages;
+        const bool tail = hole || (step + 1) * 16 * KT > ctx;  // not all of the step's keys are committed ones
+        const int key0 = step * 16 * KT;
+        const int there = hole ? 0 : total;  // keys from here on are not seen by anybody
+        const int left = there - key0 - lg * 4;  // those of them from the lane's first key on
+
+        f32x4 s[NC][KT];
+        each<NC * KT>([&](auto x) { s[decltype(x)::value / KT][decltype(x)::value % KT] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
+        u32x4 q_now[NC], q_next[NC];
+        each<NC>([&](auto ct) { q_next[decltype(ct)::value] = query(decltype(ct)::value, 0); });
+        each<QS>([&](auto xc) {
+            constexpr int i = decltype(xc)::value;
+            each<NC>([&](auto ctc) {
+                constexpr int ct = decltype(ctc)::value;
+                q_now[ct] = q_next[ct];
+                if constexpr (i + 1 < QS) q_next[ct] = query(ct, i + 1);
+            });
+            u32x4 key[KT];  // operands of this part of the heads
+            each<KT>([&](auto ktc) {
+                constexpr int kt = decltype(ktc)::value;
+                if constexpr (kCodes) {
+                    const u32x2 a = widen<KIND>(kf[kt][i / 2][i % 2 * 2]), c = widen<KIND>(kf[kt][i / 2][i % 2 * 2 + 1]);
+                    key[kt] = u32x4{a[0], a[1], c[0], c[1]};
+                } else {
+                    key[kt] = kf[kt][i];
+                }
+            });
+            each<NC>([&](auto ctc) {
+                constexpr int ct = decltype(ctc)::value;
+                each<KT>([&](auto ktc) {
+                    constexpr int kt = decltype(ktc)::value;
+                    s[ct][kt] = mma_kind<KIND>(key[kt], q_now[ct], s[ct][kt]);
+                });
+            });
+            if constexpr (NC > 1) __builtin_amdgcn_sched_barrier(0);  // (the compiler would fetch all queries first)
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kCodes) {
+            each<KT>([&](auto ktc) {
+                constexpr int kt = decltype(ktc)::value;
+                each<NC>([&](auto ct) { s[decltype(ct)::value][kt] *= ks[kt]; });
+            });
+            if (tail)  // scales of rows past the end may be anything
+                each<KT * 4>([&](auto x) {
+                    constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
+                    if (kt * 16 + e >= left) vs[kt][e] = 0.0f;
+                });
+            float most = 0.0f;
+            each<KT * 4>([&](auto x) { most = fmaxf(most, vs[decltype(x)::value / 4][decltype(x)::value % 4]); });
+            most = max_groups(most);
+            // exponent above the largest: scale * 2^-here < 1
+            const int here = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(most) >> 23) - 126);
+            const int above = max(lift, min(here, 127));
+            each<NC>([&](auto ct) { pin(decltype(ct)::value); });
+            if (above != lift) {
+                const float down = ldexpf(1.0f, max(lift - above, -140));
+                each<NC * DT>([&](auto x) { o[decltype(x)::value / DT][decltype(x)::value % DT] *= down; });
+                lift = above;
+                each<NC>([&](auto ct) { pin(decltype(ct)::value); });
+            }
+            const float up = ldexpf(1.0f, kLiftBits - lift);
+            each<KT>([&](auto kt) { vs[decltype(kt)::value] *= up; });
+        }
+        if (more) load_k(next_block, next);
+        __builtin_amdgcn_sched_barrier(0);
+
+        u32x4 p[NC][NP];
+        uint64_t vis[NC];  // keys of the step that the column sees, from the lane's first on
+        each<NC>([&](auto ctc) {
+            constexpr int ct = decltype(ctc)::value;
+            vis[ct] = ~(uint64_t)0;
+            if (tail) {
+                const int page0 = key0 & ~(kPage - 1), d0 = page0 - ctx;  // first key of the page, as a drafted token
+                const int i = token[ct], from = max(d0, 0);               // first drafted token of the page
+                uint64_t bits = 0;
+                if (i < n && from < n) {
+                    if (g.tree) {
+                        const uint64_t* row = g.tree + (int64_t)(start + i) * g.mask_words;
+                        const int w = from >> 6, r = from & 63;
+                        if (w < g.mask_words) bits = row[w] >> r;
+                        if (r && w + 1 < g.mask_words) bits |= row[w + 1] << (64 - r);
+                    } else {
+                        const int c = i + 1 - from;
+                        bits = c <= 0 ? 0 : c >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << c) - 1;
+                    }
+                    if (n - from < 64) bits &= ((uint64_t)1 << (n - from)) - 1;
+                }
+                // below them the committed keys
+                uint64_t v = d0 >= 0 ? bits : d0 <= -kPage ? ~(uint64_t)0 : (((uint64_t)1 << -d0) - 1) | bits << -d0;
+                if (there - page0 < 64) v &= there > page0 ? ((uint64_t)1 << (there - page0)) - 1 : 0;
+                if (i >= n) v = 0;
+                vis[ct] = v >> (key0 - page0 + lg * 4);
+                each<KT * 4>([&](auto x) {
+                    constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
+                    if (!(vis[ct] & (uint64_t)1 << (kt * 16 + e))) s[ct][kt][e] = -INFINITY;
+                });
+            }
+            float top = -INFINITY;
+            each<KT * 4>([&](auto x) { top = fmaxf(top, s[ct][decltype(x)::value / 4][decltype(x)::value % 4]); });
+            top = max_groups(top) * mult[ct];
+            pin(ct);
+            if (__any(top - m[ct] > kSlack)) {  // (never where top is -infinity)
+                const float up = fmaxf(m[ct], top), alpha = pow2(m[ct] - (up == -INFINITY ? 0.0f : up));
+                m[ct] = up;
+                l[ct] *= alpha;
+                each<DT>([&](auto dt) { o[ct][decltype(dt)::value] *= alpha; });
+                pin(ct);
+            }
+            const float base = m[ct] == -INFINITY ? 0.0f : m[ct];
+            float sum = 0.0f;
+            each<KT * 4>([&](auto x) {
+                constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
+                const float y = pow2(__builtin_fmaf(s[ct][kt][e], mult[ct], -base));
+                sum += y;
+                s[ct][kt][e] = kCodes ? y * vs[kt][e] : y;
+            });
+            if (kCodes && tail)  // 0 times a scale that is not a number
+                each<KT * 4>([&](auto x) {
+                    constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
+                    if (!(vis[ct] & (uint64_t)1 << (kt * 16 + e))) s[ct][kt][e] = 0.0f;
+                });
+            l[ct] += sum;
+            // tiles to operand pieces: 16-bit ones hold two tiles' keys
+            if constexpr (KIND == kF32) {
+                each<KT>([&](auto kt) { p[ct][decltype(kt)::value] = __builtin_bit_cast(u32x4, s[ct][decltype(kt)::value]); });
+            } else {
+                each<NP * 4>([&](auto x) {
+                    constexpr int i = decltype(x)::value / 4, w = decltype(x)::value % 4;
+                    const float lo = s[ct][2 * i + w / 2][(w & 1) * 2], hi = s[ct][2 * i + w / 2][(w & 1) * 2 + 1];
+                    p[ct][i][w] = kCodes ? pack_f16(lo, hi) : pack_bf16(lo, hi);
+                });
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+
+        each<NC>([&](auto ct) { pin(decltype(ct)::value); });
+        if (tail) {
+            // Values of rows past the end may be anything: zeros.  (Int8 codes are finite whatever they are.)  Piece word w of
+            // 16-bit kinds holds keys 2 (w%2), +1 of the group in tile 2i + w/2; of 8-bit ones the four keys of tile w.
+            auto row_there = [&](int kt, int e) { return kt * 16 + e < left; };
+            bool odd = false;  // a value that is not finite, of a key that some columns may not see
+            each<DT * NV * 4>([&](auto xc) {
+                constexpr int x = decltype(xc)::value, dt = x / (NV * 4), i = x / 4 % NV, w = x % 4;
+                uint32_t y = vf[dt][i][w];
+                if constexpr (KIND == kF32) {
+                    if (!row_there(i, w)) y = 0;
+                    odd = odd || (y & 0x7F800000u) == 0x7F800000u;
+                } else if constexpr (KIND == kBf16) {
+                    if (!row_there(2 * i + w / 2, (w & 1) * 2)) y &= 0xFFFF0000u;
+                    if (!row_there(2 * i + w / 2, (w & 1) * 2 + 1)) y &= 0xFFFFu;
+                    odd = odd || (y & 0x7F80u) == 0x7F80u || (y & 0x7F800000u) == 0x7F800000u;
+                } else if constexpr (KIND == kFp8) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!row_there(w, e)) y &= ~(0xFFu << 8 * e);
+                }
+                vf[dt][i][w] = y;
+                if constexpr (x % (NV * 4) == NV * 4 - 1) __builtin_amdgcn_sched_barrier(0);
+            });
+            // 0 times what is not finite would reach columns that do not see the key: such values are taken out, and
+            // counted per kind with the columns that do see them.
+            if constexpr (!kCodes) {
+                if (__any(odd)) {
+                    for (int kind = 0; kind < 3; ++kind) {  // +infinity, -infinity, NaN
+                        auto is = [&](uint32_t bits) {      // fp32 bits
+                            return kind == 0 ? bits == 0x7F800000u : kind == 1 ? bits == 0xFF800000u : (bits & 0x7FFFFFFFu) > 0x7F800000u;
+                        };
+                        each<DT * NC>([&](auto xc) {
+                            constexpr int dt = decltype(xc)::value / NC, ct = decltype(xc)::value % NC;
+                            f32x4 count = {0.0f, 0.0f, 0.0f, 0.0f};
+                            each<NV>([&](auto ic) {
+                                constexpr int i = decltype(ic)::value;
+                                u32x4 mark, seen;
+                                each<4>([&](auto wc) {
+                                    constexpr int w = decltype(wc)::value;
+                                    auto sees = [&](int kt, int e) { return (vis[ct] & (uint64_t)1 << (kt * 16 + e)) != 0; };
+                                    const uint32_t y = vf[dt][i][w];
+                                    if constexpr (KIND == kF32) {
+                                        mark[w] = is(y) ? 0x3F800000u : 0u;
+                                        seen[w] = sees(i, w) ? 0x3F800000u : 0u;
+                                    } else {
+                                        mark[w] = (is(y << 16) ? 0x3F80u : 0u) | (is(y & 0xFFFF0000u) ? 0x3F800000u : 0u);
+                                        seen[w] = (sees(2 * i + w / 2, (w & 1) * 2) ? 0x3F80u : 0u) |
+                                                  (sees(2 * i + w / 2, (w & 1) * 2 + 1) ? 0x3F800000u : 0u);
+                                    }
+                                });
+                                count = mma_kind<KIND>(mark, seen, count);
+                            });
+                            each<4>([&](auto e) {
+                                if (count[decltype(e)::value] > 0.0f)
+                                    o[ct][dt][decltype(e)::value] += kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                            });
+                            __builtin_amdgcn_sched_barrier(0);
+                        });
+                    }
+                    each<DT * NV * 4>([&](auto xc) {
+                        constexpr int x = decltype(xc)::value, dt = x / (NV * 4), i = x / 4 % NV, w = x % 4;
+                        uint32_t y = vf[dt][i][w];
+                        if constexpr (KIND == kF32) {
+                            if ((y & 0x7F800000u) == 0x7F800000u) y = 0;
+                        } else {
+                            if ((y & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
+                            if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
+                        }
+                        vf[dt][i][w] = y;
+                    });
+                }
+            }
+            each<NC>([&](auto ct) { pin(decltype(ct)::value); });
+        }
+        if (more) load_vs(next_block);
+        each<DT>([&](auto dtc) {
+            constexpr int dt = decltype(dtc)::value;
+            if constexpr (kCodes) {
+                u32x4 lo, hi;
+                fragments(vf[dt][0], lo, hi);
+                each<NC>([&](auto ct) { o[decltype(ct)::value][dt] = mma_kind<KIND>(lo, p[decltype(ct)::value][0], o[decltype(ct)::value][dt]); });
+                each<NC>([&](auto ct) { o[decltype(ct)::value][dt] = mma_kind<KIND>(hi, p[decltype(ct)::value][1], o[decltype(ct)::value][dt]); });
+            } else {
+                each<NV>([&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    each<NC>([&](auto ct) { o[decltype(ct)::value][dt] = mma_kind<KIND>(vf[dt][i], p[decltype(ct)::value][i], o[decltype(ct)::value][dt]); });
+                });
+            }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) each<DT>([&](auto dt) { load_v(next_block, next, dt); });
+        __builtin_amdgcn_sched_barrier(0);
+        step = next;
+        page = next_page;
+    }
+
+    // ---- results ----
+    if constexpr (kCodes) {
+        const float down = ldexpf(1.0f, max(lift - kLiftBits, -140));
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[ct][dt] *= down;
+    }
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct) l[ct] = sum_groups(l[ct]);
+
+    const bool direct = g.nsplit == 1;
+    auto put = [&](int c, int d, f32x4 x, float total_l) {  // four consecutive elements of column c
+        const int64_t t = start + c / g.G, head = h * g.G + c % g.G;
+        if (!direct) {
+            *(f32x4*)(g.part_o + (((int64_t)split * g.T + t) * g.heads + head) * D + d) = x;
+            return;
+        }
+        const float r = total_l != 0.0f ? 1.0f / total_l : 0.0f;
+        char* dst = g.out + (t * g.ot + head * g.oh + d) * kEsz;
+        if constexpr (KIND == kF32) *(f32x4*)dst = x * r;
+        else *(u32x2*)dst = u32x2{pack_bf16(x[0] * r, x[1] * r), pack_bf16(x[2] * r, x[3] * r)};
+    };
+    auto put_sums = [&](int c, float mm, float ll) {
+        const int64_t t = start + c / g.G, head = h * g.G + c % g.G;
+        if (!direct) {
+            float* ml = g.part_ml + (((int64_t)split * g.T + t) * g.heads + head) * 2;
+            ml[0] = mm;
+            ml[1] = ll;
+        } else if (g.lse) {
+            g.lse[t * g.heads + head] = ll == 0.0f ? -INFINITY : (mm + __log2f(ll)) * 0.693147180559945309417f;
+        }
+    };
+    if constexpr (COLS) {
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) {
+            const int c = col0 + ct * 16 + lr;
+            if (c >= C) continue;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) put(c, dt * 16 + lg * 4, o[ct][dt], l[ct]);
+            if (lg == 0) put_sums(c, m[ct], l[ct]);
+        }
+    } else {
+        // The four wavefronts had different keys: join them, 32 elements of the columns at a time.
+        float(*sums)[16 * NC][kRow] = (float(*)[16 * NC][kRow])lds;
+        __shared__ float mls[4][16 * NC][2];
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct)
+            if (lg == 0) {
+                mls[wave][ct * 16 + lr][0] = m[ct];
+                mls[wave][ct * 16 + lr][1] = l[ct];
+            }
+        __syncthreads();
+        float factor[NC];
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) {
+            const int c = ct * 16 + lr;
+            const float top = fmaxf(fmaxf(mls[0][c][0], mls[1][c][0]), fmaxf(mls[2][c][0], mls[3][c][0]));
+            factor[ct] = pow2(m[ct] - (top == -INFINITY ? 0.0f : top));
+        }
+        auto joined = [&](int c, float& top) {
+            top = fmaxf(fmaxf(mls[0][c][0], mls[1][c][0]), fmaxf(mls[2][c][0], mls[3][c][0]));
+            const float base = top == -INFINITY ? 0.0f : top;
+            float ll = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) ll += mls[w][c][1] * pow2(mls[w][c][0] - base);
+            return ll;
+        };
+#pragma unroll
+        for (int pass = 0; pass < D / 32; ++pass) {
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) *(f32x4*)&sums[wave][ct * 16 + lr][i * 16 + lg * 4] = o[ct][pass * 2 + i] * factor[ct];
+            __syncthreads();
+            for (int i = tid; i < 16 * NC * 8; i += 256) {
+                const int c = i / 8, d = i % 8 * 4;
+                if (col0 + c < C) {
+                    f32x4 x = *(f32x4*)&sums[0][c][d];
+#pragma unroll
+                    for (int w = 1; w < 4; ++w) x += *(f32x4*)&sums[w][c][d];
+                    float top;
+                    put(col0 + c, pass * 32 + d, x, joined(c, top));
+                }
+            }
+            __syncthreads();
+        }
+        if (tid < 16 * NC && col0 + tid < C) {
+            float top;
+            const float ll = joined(tid, top);
+            put_sums(col0 + tid, top, ll);
+        }
+    }
+}
+
+template <int D, int KIND>
+static void attend_wide(const Shares& r, const AttendArgs& g, hipStream_t st)
+{
+    const int64_t sets = ((int64_t)g.kv_heads * g.B * r.nsplit + 7) / 8 * 8;
+    const dim3 grid((unsigned)(sets * r.groups)), block(256);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
+    if (r.cols) {
+        if constexpr (D <= 128) r.nc == 2 ? go(attend_kernel<D, KIND, 2, true>) : go(attend_kernel<D, KIND, 4, true>);
+        else go(attend_kernel<D, KIND, 2, true>);
+    } else {
+        if (r.nc == 1) go(attend_kernel<D, KIND, 1, false>);
+        else if (r.nc == 2) go(attend_kernel<D, KIND, 2, false>);
+        else if constexpr (D <= 128) go(attend_kernel<D, KIND, 4, false>);
+    }
+}
+
+template <int KIND>
+static void attend_kind(int D, const Shares& r, const AttendArgs& g, hipStream_t st)
+{
+    if (D == 64) attend_wide<64, KIND>(r, g, st);
+    else if (D == 128) attend_wide<128, KIND>(r, g, st);
+    else attend_wide<256, KIND>(r, g, st);
+}
+
+void attend_bf16(int D, const Shares& r, const AttendArgs& g, hipStream_t st);
+void attend_int8(int D, const Shares& r, const AttendArgs& g, hipStream_t st);
+void attend_fp8(int D, const Shares& r, const AttendArgs& g, hipStream_t st);
+void attend_f32(int D, const Shares& r, const AttendArgs& g, hipStream_t st);
+
+}  // namespace mmoe
