@@ -144,7 +144,8 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     const int step1 = min(split == active - 1 ? all_pages * kSteps : (split + 1) * g.chunk * kSteps, (limit + 16 * KT - 1) / (16 * KT));
 
     constexpr int64_t kBlock = (int64_t)kPage * D * L::kBytes;
-    const int32_t* table = g.pages + (int64_t)b * g.max_pages;
+    // (constant address space: scalar loads, which the counts of the vector loads in flight do not see)
+    const auto* table = (const __attribute__((address_space(4))) int32_t*)(g.pages + (int64_t)b * g.max_pages);
     // Page and head of a step.  A page number outside the cache is page 0 with `hole` set: its keys are not seen.
     auto page_of = [&](int step) { return __builtin_amdgcn_readfirstlane(table[step / kSteps]); };
     auto block_of = [&](int page) { return (int64_t)((unsigned)page < (unsigned)g.n_pages ? page : 0) * g.kv_heads + h; };
@@ -254,8 +255,10 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     while (works && step < step1) {
         const int next = step + kStride;
         const bool more = next < step1;
-        const int next_page = more ? page_of(next) : 0;
+        // What is loaded ahead is loaded in every iteration, the last one's own step again: behind a branch the waits could not count.
+        const int next_page = page_of(more ? next : step);
         const int64_t next_block = block_of(next_page);
+        const int ahead = more ? next : step;
         const bool hole = (unsigned)page >= (unsigned)g.n_pages;
         const bool tail = hole || (step + 1) * 16 * KT > ctx;  // not all of the step's keys are committed ones
         const int key0 = step * 16 * KT;
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             const float up = ldexpf(1.0f, kLiftBits - lift);
             each<KT>([&](auto kt) { vs[decltype(kt)::value] *= up; });
         }
-        if (more) load_k(next_block, next);
+        load_k(next_block, ahead);
         __builtin_amdgcn_sched_barrier(0);
 
         u32x4 p[NC][NP];
@@ -466,7 +469,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             }
             each<NC>([&](auto ct) { pin(decltype(ct)::value); });
         }
-        if (more) load_vs(next_block);
+        load_vs(next_block);
         each<DT>([&](auto dtc) {
             constexpr int dt = decltype(dtc)::value;
             if constexpr (kCodes) {
@@ -482,7 +485,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             }
         });
         __builtin_amdgcn_sched_barrier(0);
-        if (more) each<DT>([&](auto dt) { load_v(next_block, next, dt); });
+        each<DT>([&](auto dt) { load_v(next_block, ahead, dt); });
         __builtin_amdgcn_sched_barrier(0);
         step = next;
         page = next_page;
