@@ -4,20 +4,44 @@
 
 namespace mmoe {
 
-// Joins the splits of a request's keys: a wavefront takes a (token, head).
+constexpr int kLeastPages = 16;   // of a share
+constexpr int kMaxShares = 4096;
+
+// Joins the parts of a request that several shares have: a wavefront takes a (token, head).
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 {
-    const int per = (min(g.max_drafts, g.T) * g.heads + 3) / 4, b = blockIdx.x / per;
-    const int start = g.starts[b], n = min(min(g.starts[b + 1], g.T) - start, g.max_drafts), ctx = g.ctx[b];
-    const int row = blockIdx.x % per * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;  // token of the request, head
-    if (start < 0 || ctx < 0 || row >= n * g.heads) return;
-    const int64_t t = start + row / g.heads, head = row % g.heads;
-    const int total = (int)min((int64_t)ctx + n, (int64_t)g.max_pages * kPage);
-    const int active = min(g.nsplit, max(1, ((total + kPage - 1) / kPage + g.chunk - 1) / g.chunk));
-    const int64_t at = t * g.heads + head, all = (int64_t)g.T * g.heads;
+    __shared__ int sums[256][2];
+    const int tid = threadIdx.x, per = (min(g.max_drafts, g.T) * g.heads + 3) / 4, b = blockIdx.x / per;
+    const Request r = request_of(g, b);
+    const int row = blockIdx.x % per * 4 + (tid >> 6), lane = tid & 63;  // token of the request, head
+    if (blockIdx.x % per * 4 >= r.n * g.heads) return;  // uniform
+    int before = 0, all = 0;
+    for (int i = tid; i < g.B; i += 256) {
+        const int pages = request_of(g, i).pages;
+        all += pages;
+        if (i < b) before += pages;
+    }
+#define MMOE_JOIN(OFF) all += lane_xor<OFF>(all), before += lane_xor<OFF>(before)
+    MMOE_JOIN(1); MMOE_JOIN(2); MMOE_JOIN(4); MMOE_JOIN(8); MMOE_JOIN(16); MMOE_JOIN(32);
+#undef MMOE_JOIN
+    if (lane == 0) sums[tid >> 6][0] = all, sums[tid >> 6][1] = before;
+    __syncthreads();
+    const int64_t P = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], p0 = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
+    if (row >= r.n * g.heads || !r.pages) return;
+    // shares of the request's first and last page
+    const int w0 = (int)(((p0 + 1) * g.shares - 1) / P), w1 = (int)(((p0 + r.pages) * g.shares - 1) / P);
+    if (w0 == w1) return;  // written by the share that has it all
+    const int64_t t = r.start + row / g.heads;
+    const int head = row % g.heads, h = head / g.G, c = row / g.heads * g.G + head % g.G;
+    auto part = [&](int w) {
+        const int slot = w == w0 && share_start(P, g.shares, w) < p0 ? 1 : 0;
+        return (((int64_t)w * 2 + slot) * g.kv_heads + h) * g.columns + c;
+    };
+    auto has = [&](int w) { return share_start(P, g.shares, w) < share_start(P, g.shares, w + 1); };
     float top = -INFINITY;
-    for (int s = lane; s < active; s += 64) top = fmaxf(top, g.part_ml[(s * all + at) * 2]);
+    for (int w = w0 + lane; w <= w1; w += 64)
+        if (has(w)) top = fmaxf(top, g.part_ml[part(w) * 2]);
 #define MMOE_JOIN(OFF) top = fmaxf(top, lane_xor<OFF>(top))
     MMOE_JOIN(1); MMOE_JOIN(2); MMOE_JOIN(4); MMOE_JOIN(8); MMOE_JOIN(16); MMOE_JOIN(32);
 #undef MMOE_JOIN
@@ -26,23 +50,26 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
     float x[kPer], l = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
-    for (int s = 0; s < active; ++s) {
-        const float w = pow2(g.part_ml[(s * all + at) * 2] - base);
-        l += w * g.part_ml[(s * all + at) * 2 + 1];
+#pragma unroll 4
+    for (int w = w0; w <= w1; ++w) {
+        if (!has(w)) continue;
+        const int64_t at = part(w);
+        const float f = pow2(g.part_ml[at * 2] - base);
+        l += f * g.part_ml[at * 2 + 1];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i] += w * g.part_o[(s * all + at) * D + i * 64 + lane];
+        for (int i = 0; i < kPer; ++i) x[i] += f * g.part_o[at * D + i * 64 + lane];
     }
-    const float r = l != 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int64_t dst = t * g.ot + head * g.oh + i * 64 + lane;
-        if (F32) ((float*)g.out)[dst] = x[i] * r;
-        else ((uint16_t*)g.out)[dst] = f32_to_bf16_bits(x[i] * r);
+        if (F32) ((float*)g.out)[dst] = x[i] * inv;
+        else ((uint16_t*)g.out)[dst] = f32_to_bf16_bits(x[i] * inv);
     }
-    if (lane == 0 && g.lse) g.lse[at] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * 0.693147180559945309417f;
+    if (lane == 0 && g.lse) g.lse[t * g.heads + head] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * 0.693147180559945309417f;
 }
 
-static Shares shares(const mmoe_attend_shape& s)
+static Shares shares_of(const mmoe_attend_shape& s)
 {
     Shares r;
     const int G = s.heads / s.cache.kv_heads, most = s.cache.head_dim > 128 ? 2 : 4;
@@ -52,52 +79,55 @@ static Shares shares(const mmoe_attend_shape& s)
     r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : 4;
     const int wide = 16 * r.nc * (r.cols ? 4 : 1);
     r.groups = (int)((C + wide - 1) / wide);
-    int64_t longest = s.max_keys ? s.max_keys : (int64_t)s.max_pages * kPage;
-    if (longest > (int64_t)s.max_pages * kPage) longest = (int64_t)s.max_pages * kPage;
-    const int64_t all = s.sum_keys ? s.sum_keys : (int64_t)s.n_requests * longest;
-    const int64_t pages = all / kPage + s.n_requests, most_pages = (longest + kPage - 1) / kPage;
-    const int64_t target = r.nc == 1 ? 1024 : 512;
-    int64_t chunk = (pages * s.cache.kv_heads * r.groups + target - 1) / target;
-    if (chunk < 16) chunk = 16;
-    int64_t n = (most_pages + chunk - 1) / chunk;
-    if (n > 256) n = 256, chunk = (most_pages + n - 1) / n;
-    if (n < 1) n = 1;
-    r.chunk = (int)chunk;
-    r.nsplit = (int)n;
+    const int64_t cap = (int64_t)s.max_pages * kPage;
+    const int64_t longest = s.max_keys && s.max_keys < cap ? s.max_keys : cap;
+    const int64_t sum = s.sum_keys ? s.sum_keys : (int64_t)s.n_requests * longest;
+    const int64_t pages = sum / kPage + s.n_requests, most_pages = (longest + kPage - 1) / kPage;
+    // workgroups that are resident at once, for each key head and column group
+    const int64_t room = 256 * (r.nc == 1 && s.cache.head_dim <= 128 ? 2 : 1), heads = (int64_t)s.cache.kv_heads * r.groups;
+    int64_t w = room / heads;
+    if (w < s.n_requests) w = s.n_requests;
+    if (w > pages / kLeastPages) w = pages / kLeastPages;
+    if (w > kMaxShares) w = kMaxShares;
+    // One workgroup to a request where the longest request is not what the call would wait for.
+    const int64_t rounds = (s.n_requests * heads + room - 1) / room;
+    const bool even = most_pages <= kLeastPages || most_pages * room <= pages * heads + (rounds > 1 ? pages * heads / 4 : 0);
+    r.shares = even || s.n_requests > kMaxShared || w <= 1 || s.n_requests * (int64_t)s.max_pages >= (int64_t)1 << 30 ? 0 : (int)w;
     return r;
 }
 
 // Whether the grids' sizes fit.
 bool attend_fits(const mmoe_attend_shape& s)
 {
-    const Shares r = shares(s);
+    const Shares r = shares_of(s);
     const int64_t drafts = s.max_drafts < s.T ? s.max_drafts : s.T, most = ((int64_t)1 << 31) - 1;
     return drafts * s.heads < most && (drafts * s.heads + 3) / 4 * s.n_requests <= most &&
-           ((int64_t)s.cache.kv_heads * s.n_requests + 8) * r.groups <= most / r.nsplit;
+           ((int64_t)s.cache.kv_heads * (r.shares ? r.shares : s.n_requests) + 8) * r.groups <= most;
 }
+
+// Columns of a request at most, and rows of partial results.
+static int64_t columns_of(const mmoe_attend_shape& s) { return (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * (s.heads / s.cache.kv_heads); }
+static size_t part_rows(const mmoe_attend_shape& s, const Shares& r) { return (size_t)r.shares * 2 * s.cache.kv_heads * columns_of(s); }
 
 size_t attend_ws_bytes(const mmoe_attend_shape& s)
 {
-    const Shares r = shares(s);
-    if (r.nsplit == 1) return 256;
-    const size_t rows = (size_t)r.nsplit * s.T * s.heads;
-    return align256(rows * s.cache.head_dim * 4) + align256(rows * 8);
+    const size_t rows = part_rows(s, shares_of(s));
+    return 256 + align256(rows * s.cache.head_dim * 4) + align256(rows * 8);
 }
 
 int launch_attend(const mmoe_attend_shape& s, const void* Q, const int32_t* starts, const int32_t* ctx, const uint64_t* tree,
                   const int32_t* pages, const mmoe_cache& c, void* out, float* lse, void* ws, hipStream_t st)
 {
-    const Shares r = shares(s);
+    const Shares r = shares_of(s);
     const int64_t D = s.cache.head_dim;
-    const size_t rows = (size_t)r.nsplit * s.T * s.heads;
     AttendArgs g = {(const char*)Q, starts, ctx, tree, pages, (const char*)c.k, (const char*)c.v, c.k_scale, c.v_scale, (char*)out, lse,
-                    (float*)ws, (float*)((char*)ws + align256(rows * D * 4)),
+                    (float*)ws, (float*)((char*)ws + align256(part_rows(s, r) * D * 4)),
                     s.q_token ? s.q_token : s.heads * D, s.q_head ? s.q_head : D, s.o_token ? s.o_token : s.heads * D,
                     s.o_head ? s.o_head : D, s.T, s.n_requests, s.heads, s.cache.kv_heads, s.heads / s.cache.kv_heads, s.max_pages,
-                    s.max_drafts, s.mask_words, s.cache.n_pages, r.groups, r.nsplit, r.chunk, s.scale};
+                    s.max_drafts, s.mask_words, s.cache.n_pages, r.groups, r.shares, (int)columns_of(s), s.scale};
     const bool f32 = s.cache.dtype == MMOE_F32;
     (s.cache.format == MMOE_CACHE_INT8 ? attend_int8 : s.cache.format == MMOE_CACHE_FP8 ? attend_fp8 : f32 ? attend_f32 : attend_bf16)((int)D, r, g, st);
-    if (r.nsplit > 1) {
+    if (r.shares) {
         const int64_t drafts = s.max_drafts < s.T ? s.max_drafts : s.T;
         const dim3 grid((unsigned)((drafts * s.heads + 3) / 4 * s.n_requests)), block(256);
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };

@@ -19,11 +19,32 @@ namespace mmoe {
 enum { kBf16 = 0, kInt8 = 1, kFp8 = 2, kF32 = 3 };  // what pages hold
 
 // How a call is shared out: 16-column tiles to a wavefront, whether the wavefronts of a workgroup take different columns or
-// different keys, and splits of the keys.
+// different keys, groups of columns, and workgroups for each key head and column group: one for each request (shares 0), or
+// `shares` ones that take equal parts of all requests' pages one after the other.
 struct Shares {
-    int nc, groups, chunk, nsplit;
+    int nc, groups, shares;
     bool cols;
 };
+constexpr int kMaxShared = 4096;  // requests whose pages are shared out
+
+// The request's drafted tokens, its keys, and their pages.
+struct Request {
+    int start, n, ctx, total, pages;
+};
+template <typename G>
+__device__ __forceinline__ Request request_of(const G& g, int b)
+{
+    Request r;
+    r.start = g.starts[b];
+    r.n = min(min(g.starts[b + 1], g.T) - r.start, g.max_drafts);
+    r.ctx = g.ctx[b];
+    if (r.start < 0 || r.ctx < 0) r.n = 0;
+    r.total = r.n > 0 ? (int)min((int64_t)r.ctx + r.n, (int64_t)g.max_pages * kPage) : 0;
+    r.pages = (r.total + kPage - 1) / kPage;
+    return r;
+}
+// First page of a share.
+__device__ __forceinline__ int64_t share_start(int64_t pages, int shares, int w) { return pages * w / shares; }
 
 struct AttendArgs {
     const char* Q;
@@ -34,11 +55,12 @@ struct AttendArgs {
     const float *k_scale, *v_scale;
     char* out;
     float* lse;
-    float* part_o;   // [nsplit][T * heads][D]
-    float* part_ml;  // [nsplit][T * heads][2]
+    // a share's part of a request that it does not have all of, [shares][2][kv_heads][columns]: 0 the share's first, 1 its last
+    float* part_o;   // [D]
+    float* part_ml;  // [2]
     int64_t qt, qh, ot, oh;
     int T, B, heads, kv_heads, G, max_pages, max_drafts, mask_words, n_pages;
-    int groups, nsplit, chunk;  // column groups; splits of the keys, pages of each
+    int groups, shares, columns;  // column groups; see Shares; columns of a request at most
     float scale;
 };
 
@@ -125,23 +147,70 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     id = id / g.groups * 8 + blockIdx.x % 8;
     const int h = id % g.kv_heads;
     id /= g.kv_heads;
-    const int b = id % g.B, split = id / g.B;
-    if (split >= g.nsplit) return;
-    const int start = g.starts[b], n = min(min(g.starts[b + 1], g.T) - start, g.max_drafts), ctx = g.ctx[b];
-    const int C = n * g.G;
+    const int share = id;
+    if (share >= (g.shares ? g.shares : g.B)) return;  // uniform
+
+    constexpr int kQWaves = COLS ? 4 : 1;  // wavefronts with the same columns share them
+    constexpr int kQBytes = L::kLdsQ ? kQWaves * NC * QS * 1024 : 16;
+    constexpr int kRow = 36, kSumBytes = COLS ? 16 : 4 * 16 * NC * kRow * 4;
+    __shared__ __attribute__((aligned(16))) char lds[kQBytes > kSumBytes ? kQBytes : kSumBytes];  // queries, and at the end the join's sums
+    __shared__ float mls[COLS ? 1 : 4][16 * NC][2];
+    __shared__ int first_page[kMaxShared + 1];  // of each request among all pages (fewer than 2^30, or there are no shares)
+
+    int64_t at = 0, until = 1;  // pages of the share
+    int b = share;
+    if (g.shares) {
+        // prefix sums over the requests: a thread has a run of them
+        __shared__ int run_sum[256];
+        const int per = (g.B + 255) / 256;
+        int sum = 0;
+        for (int i = tid * per; i < min((tid + 1) * per, g.B); ++i) sum += request_of(g, i).pages;
+        run_sum[tid] = sum;
+        __syncthreads();
+        int before = 0;
+        for (int i = 0; i < tid; ++i) before += run_sum[i];
+        for (int i = tid * per; i < min((tid + 1) * per, g.B); ++i) {
+            first_page[i] = before;
+            before += request_of(g, i).pages;
+        }
+        if (tid == 255) first_page[g.B] = before;
+        __syncthreads();
+        const int64_t all = first_page[g.B];
+        at = share_start(all, g.shares, share);
+        until = share_start(all, g.shares, share + 1);
+        if (at >= until) return;  // uniform
+        int lo = 0, hi = g.B;  // the request with page `at`: the last one that starts there or before, if it has pages
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (first_page[mid] <= at) lo = mid;
+            else hi = mid;
+        }
+        b = __builtin_amdgcn_readfirstlane(lo);
+    }
+    const int64_t share_at = at;
+  for (; at < until; ++b) {  // requests of the share
+    const Request r = request_of(g, b);
+    const int start = r.start, n = r.n, ctx = r.ctx, total = r.total, C = n * g.G;
     constexpr int kWide = COLS ? 64 * NC : 16 * NC;
-    if (start < 0 || cg * kWide >= C || ctx < 0) return;  // uniform
-    const int total = (int)min((int64_t)ctx + n, (int64_t)g.max_pages * kPage);
-    const int all_pages = (total + kPage - 1) / kPage;
-    const int active = min(g.nsplit, max(1, (all_pages + g.chunk - 1) / g.chunk));
-    if (split >= active) return;
+    // pages of the request that are the share's; `slot`: where its part goes, -1 if it is all of the request
+    int page0 = 0, page1 = r.pages, slot = -1;
+    if (g.shares) {
+        const int64_t first = first_page[b];
+        page0 = (int)(at - first);
+        page1 = (int)min(until - first, (int64_t)r.pages);
+        if (page0 > 0 || page1 < r.pages) slot = at == share_at ? 0 : 1;
+        at = first + page1;
+    } else {
+        at = until;
+    }
+    if (cg * kWide >= C) continue;  // uniform
     const int col0 = cg * kWide + (COLS ? wave * 16 * NC : 0);
 
     // what the last column of these sees at most
     const int last_token = min(C - 1, cg * kWide + kWide - 1) / g.G;
     const int limit = g.tree ? total : (int)min((int64_t)total, (int64_t)ctx + last_token + 1);
-    const int step0 = split * g.chunk * kSteps;
-    const int step1 = min(split == active - 1 ? all_pages * kSteps : (split + 1) * g.chunk * kSteps, (limit + 16 * KT - 1) / (16 * KT));
+    const int step0 = page0 * kSteps;
+    const int step1 = min(page1 * kSteps, (limit + 16 * KT - 1) / (16 * KT));
 
     constexpr int64_t kBlock = (int64_t)kPage * D * L::kBytes;
     // (constant address space: scalar loads, which the counts of the vector loads in flight do not see)
@@ -182,10 +251,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     }
 
     // ---- queries ----
-    constexpr int kQWaves = COLS ? 4 : 1;  // wavefronts with the same columns share them
-    constexpr int kQBytes = L::kLdsQ ? kQWaves * NC * QS * 1024 : 16;
-    constexpr int kRow = 36, kSumBytes = COLS ? 16 : 4 * 16 * NC * kRow * 4;
-    __shared__ __attribute__((aligned(16))) char lds[kQBytes > kSumBytes ? kQBytes : kSumBytes];  // queries, and at the end the join's sums
+    if constexpr (L::kLdsQ || !COLS) __syncthreads();  // the request before is done with the LDS
     char* const lds_q = lds + (COLS ? wave * NC * QS * 1024 : 0) + lane * 16;
     u32x4 q_reg[L::kLdsQ ? 1 : QS];
     float mult[NC];  // of the scores, in base 2; positive
@@ -502,11 +568,12 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
 #pragma unroll
     for (int ct = 0; ct < NC; ++ct) l[ct] = sum_groups(l[ct]);
 
-    const bool direct = g.nsplit == 1;
+    const bool direct = slot < 0;
+    const int64_t part = (((int64_t)share * 2 + slot) * g.kv_heads + h) * g.columns;
     auto put = [&](int c, int d, f32x4 x, float total_l) {  // four consecutive elements of column c
         const int64_t t = start + c / g.G, head = h * g.G + c % g.G;
         if (!direct) {
-            *(f32x4*)(g.part_o + (((int64_t)split * g.T + t) * g.heads + head) * D + d) = x;
+            *(f32x4*)(g.part_o + (part + c) * D + d) = x;
             return;
         }
         const float r = total_l != 0.0f ? 1.0f / total_l : 0.0f;
@@ -517,7 +584,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     auto put_sums = [&](int c, float mm, float ll) {
         const int64_t t = start + c / g.G, head = h * g.G + c % g.G;
         if (!direct) {
-            float* ml = g.part_ml + (((int64_t)split * g.T + t) * g.heads + head) * 2;
+            float* ml = g.part_ml + (part + c) * 2;
             ml[0] = mm;
             ml[1] = ll;
         } else if (g.lse) {
@@ -536,7 +603,6 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     } else {
         // The four wavefronts had different keys: join them, 32 elements of the columns at a time.
         float(*sums)[16 * NC][kRow] = (float(*)[16 * NC][kRow])lds;
-        __shared__ float mls[4][16 * NC][2];
 #pragma unroll
         for (int ct = 0; ct < NC; ++ct)
             if (lg == 0) {
@@ -584,12 +650,13 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             put_sums(col0 + tid, top, ll);
         }
     }
+  }
 }
 
 template <int D, int KIND>
 static void attend_wide(const Shares& r, const AttendArgs& g, hipStream_t st)
 {
-    const int64_t sets = ((int64_t)g.kv_heads * g.B * r.nsplit + 7) / 8 * 8;
+    const int64_t sets = ((int64_t)g.kv_heads * (r.shares ? r.shares : g.B) + 7) / 8 * 8;
     const dim3 grid((unsigned)(sets * r.groups)), block(256);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
     if (r.cols) {
