@@ -27,21 +27,21 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 #undef MMOE_JOIN
     if (lane == 0) sums[tid >> 6][0] = all, sums[tid >> 6][1] = before;
     __syncthreads();
-    const int64_t P = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], p0 = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
+    const int P = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], p0 = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
     if (row >= r.n * g.heads || !r.pages) return;
     // shares of the request's first and last page
-    const int w0 = (int)(((p0 + 1) * g.shares - 1) / P), w1 = (int)(((p0 + r.pages) * g.shares - 1) / P);
+    const Cut cut(P, g.shares);
+    const int w0 = cut.of(p0), w1 = cut.of(p0 + r.pages - 1);
     if (w0 == w1) return;  // written by the share that has it all
     const int64_t t = r.start + row / g.heads;
     const int head = row % g.heads, h = head / g.G, c = row / g.heads * g.G + head % g.G;
     auto part = [&](int w) {
-        const int slot = w == w0 && share_start(P, g.shares, w) < p0 ? 1 : 0;
+        const int slot = w == w0 && cut.start(w) < p0 ? 1 : 0;
         return (((int64_t)w * 2 + slot) * g.kv_heads + h) * g.columns + c;
     };
-    auto has = [&](int w) { return share_start(P, g.shares, w) < share_start(P, g.shares, w + 1); };
     float top = -INFINITY;
     for (int w = w0 + lane; w <= w1; w += 64)
-        if (has(w)) top = fmaxf(top, g.part_ml[part(w) * 2]);
+        top = fmaxf(top, g.part_ml[part(w) * 2]);
 #define MMOE_JOIN(OFF) top = fmaxf(top, lane_xor<OFF>(top))
     MMOE_JOIN(1); MMOE_JOIN(2); MMOE_JOIN(4); MMOE_JOIN(8); MMOE_JOIN(16); MMOE_JOIN(32);
 #undef MMOE_JOIN
@@ -52,7 +52,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
     for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
 #pragma unroll 4
     for (int w = w0; w <= w1; ++w) {
-        if (!has(w)) continue;
         const int64_t at = part(w);
         const float f = pow2(g.part_ml[at * 2] - base);
         l += f * g.part_ml[at * 2 + 1];
@@ -76,7 +75,7 @@ static Shares shares_of(const mmoe_attend_shape& s)
     const int64_t C = (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * G;
     r.cols = C > 16 * most;
     const int64_t per = r.cols ? (C + 3) / 4 : C;
-    r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : 4;
+    r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : !r.cols && per <= 48 ? 3 : 4;
     const int wide = 16 * r.nc * (r.cols ? 4 : 1);
     r.groups = (int)((C + wide - 1) / wide);
     const int64_t cap = (int64_t)s.max_pages * kPage;

@@ -43,8 +43,17 @@ __device__ __forceinline__ Request request_of(const G& g, int b)
     r.pages = (r.total + kPage - 1) / kPage;
     return r;
 }
-// First page of a share.
-__device__ __forceinline__ int64_t share_start(int64_t pages, int shares, int w) { return pages * w / shares; }
+// Shares of `pages` pages: the first `more` of them have each + 1.
+struct Cut {
+    int each, more;
+    __device__ Cut(int pages, int shares) : each(pages / shares), more(pages % shares) {}
+    __device__ int start(int w) const { return w * each + min(w, more); }
+    __device__ int of(int page) const
+    {
+        const int lead = more * (each + 1);
+        return page < lead ? page / (each + 1) : more + (page - lead) / each;
+    }
+};
 
 struct AttendArgs {
     const char* Q;
@@ -152,32 +161,43 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
 
     constexpr int kQWaves = COLS ? 4 : 1;  // wavefronts with the same columns share them
     constexpr int kQBytes = L::kLdsQ ? kQWaves * NC * QS * 1024 : 16;
-    constexpr int kRow = 36, kSumBytes = COLS ? 16 : 4 * 16 * NC * kRow * 4;
+    constexpr int kRow = 36, kSumBytes = COLS ? 16 : 2 * 4 * 16 * NC * kRow * 4;
     __shared__ __attribute__((aligned(16))) char lds[kQBytes > kSumBytes ? kQBytes : kSumBytes];  // queries, and at the end the join's sums
     __shared__ float mls[COLS ? 1 : 4][16 * NC][2];
     __shared__ int first_page[kMaxShared + 1];  // of each request among all pages (fewer than 2^30, or there are no shares)
 
-    int64_t at = 0, until = 1;  // pages of the share
+    int at = 0, until = 1;  // pages of the share
     int b = share;
     if (g.shares) {
         // prefix sums over the requests: a thread has a run of them
-        __shared__ int run_sum[256];
+        __shared__ int wave_sum[4];
         const int per = (g.B + 255) / 256;
         int sum = 0;
         for (int i = tid * per; i < min((tid + 1) * per, g.B); ++i) sum += request_of(g, i).pages;
-        run_sum[tid] = sum;
+        int before = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const int up = __shfl_up(before, off);
+            if (lane >= off) before += up;
+        }
+        if (lane == 63) wave_sum[wave] = before;
         __syncthreads();
-        int before = 0;
-        for (int i = 0; i < tid; ++i) before += run_sum[i];
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) before += wave_sum[w];
+            all += wave_sum[w];
+        }
+        before -= sum;
         for (int i = tid * per; i < min((tid + 1) * per, g.B); ++i) {
             first_page[i] = before;
             before += request_of(g, i).pages;
         }
-        if (tid == 255) first_page[g.B] = before;
+        if (tid == 0) first_page[g.B] = all;
         __syncthreads();
-        const int64_t all = first_page[g.B];
-        at = share_start(all, g.shares, share);
-        until = share_start(all, g.shares, share + 1);
+        const Cut cut(all, g.shares);
+        at = cut.start(share);
+        until = cut.start(share + 1);
         if (at >= until) return;  // uniform
         int lo = 0, hi = g.B;  // the request with page `at`: the last one that starts there or before, if it has pages
         while (hi - lo > 1) {
@@ -187,7 +207,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         }
         b = __builtin_amdgcn_readfirstlane(lo);
     }
-    const int64_t share_at = at;
+    const int share_at = at;
   for (; at < until; ++b) {  // requests of the share
     const Request r = request_of(g, b);
     const int start = r.start, n = r.n, ctx = r.ctx, total = r.total, C = n * g.G;
@@ -195,9 +215,9 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     // pages of the request that are the share's; `slot`: where its part goes, -1 if it is all of the request
     int page0 = 0, page1 = r.pages, slot = -1;
     if (g.shares) {
-        const int64_t first = first_page[b];
-        page0 = (int)(at - first);
-        page1 = (int)min(until - first, (int64_t)r.pages);
+        const int first = __builtin_amdgcn_readfirstlane(first_page[b]);
+        page0 = at - first;
+        page1 = min(until - first, r.pages);
         if (page0 > 0 || page1 < r.pages) slot = at == share_at ? 0 : 1;
         at = first + page1;
     } else {
@@ -256,11 +276,13 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     u32x4 q_reg[L::kLdsQ ? 1 : QS];
     float mult[NC];  // of the scores, in base 2; positive
     int token[NC];   // of the request; n where the column is none
+    uint64_t word[NC];  // first 64 bits of the token's row of the tree
     each<NC>([&](auto ctc) {
         constexpr int ct = decltype(ctc)::value;
         const int c = col0 + ct * 16 + lr;
         const bool there = c < C && g.scale != 0.0f;
         token[ct] = c < C ? c / g.G : n;
+        word[ct] = g.tree && c < C ? g.tree[(int64_t)(start + token[ct]) * g.mask_words] : 0;
         const char* src = g.Q + ((int64_t)(start + (there ? c / g.G : 0)) * g.qt + (int64_t)(h * g.G + (there ? c % g.G : 0)) * g.qh) * kEsz;
         mult[ct] = g.scale != 0.0f ? fabsf(g.scale) * 1.44269504088896340736f : 1.0f;
         const uint32_t sign = g.scale < 0.0f ? (KIND == kF32 ? 0x80000000u : 0x80008000u) : 0u;
@@ -404,7 +426,8 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
                     if (g.tree) {
                         const uint64_t* row = g.tree + (int64_t)(start + i) * g.mask_words;
                         const int w = from >> 6, r = from & 63;
-                        if (w < g.mask_words) bits = row[w] >> r;
+                        if (w == 0) bits = word[ct] >> r;
+                        else if (w < g.mask_words) bits = row[w] >> r;
                         if (r && w + 1 < g.mask_words) bits |= row[w + 1] << (64 - r);
                     } else {
                         const int c = i + 1 - from;
@@ -570,85 +593,84 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
 
     const bool direct = slot < 0;
     const int64_t part = (((int64_t)share * 2 + slot) * g.kv_heads + h) * g.columns;
-    auto put = [&](int c, int d, f32x4 x, float total_l) {  // four consecutive elements of column c
-        const int64_t t = start + c / g.G, head = h * g.G + c % g.G;
-        if (!direct) {
-            *(f32x4*)(g.part_o + (part + c) * D + d) = x;
-            return;
-        }
-        const float r = total_l != 0.0f ? 1.0f / total_l : 0.0f;
-        char* dst = g.out + (t * g.ot + head * g.oh + d) * kEsz;
-        if constexpr (KIND == kF32) *(f32x4*)dst = x * r;
-        else *(u32x2*)dst = u32x2{pack_bf16(x[0] * r, x[1] * r), pack_bf16(x[2] * r, x[3] * r)};
+    // Four consecutive elements of column c, whose token and head have their place in `to`.
+    auto put = [&](int c, int64_t to, int d, f32x4 x) {
+        if (!direct) *(f32x4*)(g.part_o + (part + c) * D + d) = x;
+        else if constexpr (KIND == kF32) *(f32x4*)(g.out + (to + d) * kEsz) = x;
+        else *(u32x2*)(g.out + (to + d) * kEsz) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
     };
+    auto place = [&](int c) { return (int64_t)(start + c / g.G) * g.ot + (int64_t)(h * g.G + c % g.G) * g.oh; };
     auto put_sums = [&](int c, float mm, float ll) {
-        const int64_t t = start + c / g.G, head = h * g.G + c % g.G;
         if (!direct) {
             float* ml = g.part_ml + (part + c) * 2;
             ml[0] = mm;
             ml[1] = ll;
         } else if (g.lse) {
-            g.lse[t * g.heads + head] = ll == 0.0f ? -INFINITY : (mm + __log2f(ll)) * 0.693147180559945309417f;
+            g.lse[(int64_t)(start + c / g.G) * g.heads + h * g.G + c % g.G] = ll == 0.0f ? -INFINITY : (mm + __log2f(ll)) * 0.693147180559945309417f;
         }
     };
+    auto share_of = [&](float ll) { return !direct ? 1.0f : ll != 0.0f ? 1.0f / ll : 0.0f; };  // partial results stay sums
     if constexpr (COLS) {
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
+        each<NC>([&](auto ctc) {
+            constexpr int ct = decltype(ctc)::value;
             const int c = col0 + ct * 16 + lr;
-            if (c >= C) continue;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) put(c, dt * 16 + lg * 4, o[ct][dt], l[ct]);
-            if (lg == 0) put_sums(c, m[ct], l[ct]);
-        }
+            if (c < C) {
+                const int64_t to = place(c);
+                const float f = share_of(l[ct]);
+                each<DT>([&](auto dt) { put(c, to, decltype(dt)::value * 16 + lg * 4, o[ct][decltype(dt)::value] * f); });
+                if (lg == 0) put_sums(c, m[ct], l[ct]);
+            }
+        });
     } else {
-        // The four wavefronts had different keys: join them, 32 elements of the columns at a time.
-        float(*sums)[16 * NC][kRow] = (float(*)[16 * NC][kRow])lds;
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct)
+        // The four wavefronts had different keys: join them, 32 elements of the columns at a time, in two buffers in turn.
+        float(*sums)[4][16 * NC][kRow] = (float(*)[4][16 * NC][kRow])lds;
+        each<NC>([&](auto ctc) {
+            constexpr int ct = decltype(ctc)::value;
             if (lg == 0) {
                 mls[wave][ct * 16 + lr][0] = m[ct];
                 mls[wave][ct * 16 + lr][1] = l[ct];
             }
+        });
         __syncthreads();
-        float factor[NC];
+        if (tid < 16 * NC) {
+            float top = -INFINITY, ll = 0.0f, f[4];
 #pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            const int c = ct * 16 + lr;
-            const float top = fmaxf(fmaxf(mls[0][c][0], mls[1][c][0]), fmaxf(mls[2][c][0], mls[3][c][0]));
-            factor[ct] = pow2(m[ct] - (top == -INFINITY ? 0.0f : top));
-        }
-        auto joined = [&](int c, float& top) {
-            top = fmaxf(fmaxf(mls[0][c][0], mls[1][c][0]), fmaxf(mls[2][c][0], mls[3][c][0]));
-            const float base = top == -INFINITY ? 0.0f : top;
-            float ll = 0.0f;
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, mls[w][tid][0]);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) ll += mls[w][c][1] * pow2(mls[w][c][0] - base);
-            return ll;
-        };
-#pragma unroll
-        for (int pass = 0; pass < D / 32; ++pass) {
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) *(f32x4*)&sums[wave][ct * 16 + lr][i * 16 + lg * 4] = o[ct][pass * 2 + i] * factor[ct];
-            __syncthreads();
-            for (int i = tid; i < 16 * NC * 8; i += 256) {
-                const int c = i / 8, d = i % 8 * 4;
-                if (col0 + c < C) {
-                    f32x4 x = *(f32x4*)&sums[0][c][d];
-#pragma unroll
-                    for (int w = 1; w < 4; ++w) x += *(f32x4*)&sums[w][c][d];
-                    float top;
-                    put(col0 + c, pass * 32 + d, x, joined(c, top));
-                }
+            for (int w = 0; w < 4; ++w) {
+                f[w] = pow2(mls[w][tid][0] - (top == -INFINITY ? 0.0f : top));
+                ll += mls[w][tid][1] * f[w];
             }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mls[w][tid][0] = f[w] * share_of(ll);
+            if (col0 + tid < C) put_sums(col0 + tid, top, ll);
+        }
+        __syncthreads();
+        constexpr int kPer = (16 * NC * 8 + 255) / 256;  // of a thread: four elements of a column
+        int64_t to[kPer];
+        each<kPer>([&](auto x) {
+            const int c = (tid + decltype(x)::value * 256) / 8;
+            to[decltype(x)::value] = place(min(col0 + c, C - 1));
+        });
+        float f[NC];
+        each<NC>([&](auto ct) { f[decltype(ct)::value] = mls[wave][decltype(ct)::value * 16 + lr][0]; });
+        each<D / 32>([&](auto passc) {
+            constexpr int pass = decltype(passc)::value, buf = pass & 1;
+            each<NC * 2>([&](auto x) {
+                constexpr int ct = decltype(x)::value / 2, i = decltype(x)::value % 2;
+                *(f32x4*)&sums[buf][wave][ct * 16 + lr][i * 16 + lg * 4] = o[ct][pass * 2 + i] * f[ct];
+            });
             __syncthreads();
-        }
-        if (tid < 16 * NC && col0 + tid < C) {
-            float top;
-            const float ll = joined(tid, top);
-            put_sums(col0 + tid, top, ll);
-        }
+            each<kPer>([&](auto xc) {
+                const int i = tid + decltype(xc)::value * 256, c = i / 8, d = i % 8 * 4;
+                if (c < 16 * NC && col0 + c < C) {
+                    f32x4 x = *(f32x4*)&sums[buf][0][c][d];
+#pragma unroll
+                    for (int w = 1; w < 4; ++w) x += *(f32x4*)&sums[buf][w][c][d];
+                    put(col0 + c, to[decltype(xc)::value], pass * 32 + d, x);
+                }
+            });
+        });
     }
   }
 }
@@ -665,7 +687,7 @@ static void attend_wide(const Shares& r, const AttendArgs& g, hipStream_t st)
     } else {
         if (r.nc == 1) go(attend_kernel<D, KIND, 1, false>);
         else if (r.nc == 2) go(attend_kernel<D, KIND, 2, false>);
-        else if constexpr (D <= 128) go(attend_kernel<D, KIND, 4, false>);
+        else if constexpr (D <= 128) r.nc == 3 ? go(attend_kernel<D, KIND, 3, false>) : go(attend_kernel<D, KIND, 4, false>);
     }
 }
 
