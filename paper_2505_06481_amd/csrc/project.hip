@@ -43,61 +43,151 @@ int launch_pack_pieces(const void* in, void* out, int S, int K, int N, int Kp, i
 // ---- U = scale (X A) ----------------------------------------------------------------------------------
 // With bf16 storage U is kept as two bf16 parts, the value rounded and what that leaves, [T][2][Rp]: the second product runs
 // on the bf16 instruction with 16 bits of U, so the adapter adds no error of its own to the rounding of Y.
-// A workgroup takes 16 tokens; its four wavefronts a quarter of K each.  For every adapter among the tokens all 16 are
-// multiplied, and the tokens whose adapter it is keep the result.
-template <bool F32>
-__global__ __launch_bounds__(256) void shrink_kernel(const char* __restrict__ X, int64_t ldx, const int32_t* __restrict__ aid,
-                                                     const char* __restrict__ Ap, const float* __restrict__ scale,
-                                                     char* __restrict__ U, int T, int K, int Rp, int n)
+//
+// A workgroup takes the tokens of one adapter among a chunk of the batch, 32 at a time; its four wavefronts a quarter of K each.
+// A token is read once and an adapter once for each chunk that has tokens of it.  Adapters are numbered by `group`: their own
+// number, or, where they are more than the tokens of a chunk, that of the chunk's first token that uses it.
+struct ShrinkArgs {
+    const char *X, *Ap;
+    const int32_t* aid;
+    const float* scale;
+    char* U;
+    int64_t ldx;
+    int T, K, R, Rp, n;
+    int chunk;        // tokens
+    bool by_token;    // groups are tokens (chunks of up to kScan)
+};
+constexpr int kScan = 512;  // tokens looked through at once
+struct ShrinkLds {
+    float part[4][32][33];
+    int list[kScan];
+    int count;
+};
+
+// The tokens t0 .. t0 + count - 1 (at most kScan) with adapter a, ascending, to `list`; returns how many.  a = n stands for none.
+__device__ __forceinline__ int tokens_of(const int32_t* aid, int t0, int count, int a, int n, int* list, int* shared_count)
 {
-    constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
-    __shared__ float part[4][16][17];
-    __shared__ int of[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
-    const int t0 = blockIdx.x * 16;
-    if (tid < 16) {
-        const int a = t0 + tid < T ? aid[t0 + tid] : -1;
-        of[tid] = (unsigned)a < (unsigned)n ? a : -1;
+    // one wavefront: 64 at a time, in order
+    if (threadIdx.x < 64) {
+        int at = 0;
+        for (int i = threadIdx.x; i < (count + 63) / 64 * 64; i += 64) {
+            const int x = n && i < count ? aid[t0 + i] : -1;
+            const bool mine = i < count && ((unsigned)x < (unsigned)n ? x == a : a == n);
+            const uint64_t who = __ballot(mine);
+            if (mine) list[at + __popcll(who & (((uint64_t)1 << threadIdx.x) - 1))] = t0 + i;
+            at += __popcll(who);
+        }
+        if (threadIdx.x == 0) *shared_count = at;
     }
     __syncthreads();
-    const int slices = K * kEsz / 64, per = slices / 4;  // 64 bytes of a row each
-    const char* x = X + (int64_t)min(t0 + lr, T - 1) * ldx * kEsz + wave * per * 64 + lg * 16;
-    for (int i = 0; i < 16; ++i) {
-        const int a = of[i];
-        bool first = a >= 0;
-        for (int j = 0; j < i; ++j) first = first && of[j] != a;
-        if (!first) continue;  // uniform
-        for (int rb = 0; rb < Rp / 16; ++rb) {
-            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-            const char* w = Ap + (((int64_t)a * (Rp / 16) + rb) * slices + wave * per) * 1024 + lane * 16;
-#pragma unroll 4
-            for (int s = 0; s < per; ++s)
-                acc = mma<F32>(*(const u32x4*)(w + (int64_t)s * 1024), *(const u32x4*)(x + s * 64), acc);
-            __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*shared_count);
+}
+
+// The adapter of a group (n: none), or -1 if the group has no tokens to look for.
+__device__ __forceinline__ int adapter_of(const int32_t* aid, int t0, int count, int group, bool by_token, int n)
+{
+    if (!by_token) return group;
+    if (group >= count) return -1;
+    const int x = aid[t0 + group], a = (unsigned)x < (unsigned)n ? x : n;
+    bool first = true;  // of the tokens with this adapter
+    for (int i = threadIdx.x & 63; i < group; i += 64) {
+        const int y = aid[t0 + i];
+        if (((unsigned)y < (unsigned)n ? y : n) == a) first = false;
+    }
+    return __all(first) ? a : -1;
+}
+
+template <bool F32, int RB>
+__device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds, int a, int rb0, int cols, int at, int count)
+{
+    constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    const int slices = g.K * kEsz / 64, per = slices / 4;  // 64 bytes of a row each
+    const char* x[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[wave][lg * 4 + e][lr] = acc[e];
-            __syncthreads();
-            const int tok = tid >> 4, r = tid & 15;
-            if (of[tok] == a) {
-                const float v = (part[0][r][tok] + part[1][r][tok] + (part[2][r][tok] + part[3][r][tok])) * scale[a];
-                const int64_t at = (int64_t)(t0 + tok) * Rp * kParts + rb * 16 + r;
-                if (F32) {
-                    ((float*)U)[at] = v;
-                } else {
-                    const uint16_t hi = f32_to_bf16_bits(v);
-                    ((uint16_t*)U)[at] = hi;
-                    ((uint16_t*)U)[at + Rp] = f32_to_bf16_bits(v - bf16_bits_to_f32(hi));
-                }
+    for (int j = 0; j < 2; ++j) x[j] = g.X + (int64_t)lds.list[at + min(j * 16 + lr, count - 1)] * g.ldx * kEsz + wave * per * 64 + lg * 16;
+    const char* w = g.Ap + (((int64_t)a * (g.Rp / 16) + rb0) * slices + wave * per) * 1024 + lane * 16;
+    f32x4 acc[RB][2];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const bool two = count > 16;  // uniform
+    auto slice = [&](auto qc, int s) {  // slices s .. s + Q - 1, their loads together
+        constexpr int Q = decltype(qc)::value;
+        u32x4 xf[Q][2], wf[Q][RB];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            xf[q][0] = *(const u32x4*)(x[0] + (s + q) * 64);
+            if (two) xf[q][1] = *(const u32x4*)(x[1] + (s + q) * 64);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) wf[q][i] = *(const u32x4*)(w + ((int64_t)i * slices + s + q) * 1024);
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                acc[i][0] = mma<F32>(wf[q][i], xf[q][0], acc[i][0]);
+                if (two) acc[i][1] = mma<F32>(wf[q][i], xf[q][1], acc[i][1]);
             }
+    };
+    int s = 0;
+    for (; s + 8 <= per; s += 8) slice(std::integral_constant<int, 8>{}, s);
+    for (; s < per; s += 2) slice(std::integral_constant<int, 2>{}, s);  // (K is a multiple of 256, eight slices: per is even)
+    __syncthreads();  // the sums of the tiles before have been read
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lds.part[wave][i * 16 + lg * 4 + e][j * 16 + lr] = acc[i][j][e];
+    __syncthreads();
+    const float f = g.scale[a];
+    for (int i = tid; i < count * cols; i += 256) {  // cols: those of U from rb0 on; the padding's are zeros
+        const int tok = i / cols, r = i % cols;
+        const float v = r < RB * 16 ? (lds.part[0][r][tok] + lds.part[1][r][tok] + (lds.part[2][r][tok] + lds.part[3][r][tok])) * f : 0.0f;
+        const int64_t to = (int64_t)lds.list[at + tok] * g.Rp * kParts + rb0 * 16 + r;
+        if (F32) {
+            ((float*)g.U)[to] = v;
+        } else {
+            const uint16_t hi = f32_to_bf16_bits(v);
+            ((uint16_t*)g.U)[to] = hi;
+            ((uint16_t*)g.U)[to + g.Rp] = f32_to_bf16_bits(v - bf16_bits_to_f32(hi));
         }
     }
+}
+
+template <bool F32>
+__device__ __forceinline__ void shrink_body(const ShrinkArgs& g, ShrinkLds& lds, int group, int chunk)
+{
+    const int t0 = chunk * g.chunk, t1 = min(t0 + g.chunk, g.T);
+    const int a = adapter_of(g.aid, t0, t1 - t0, group, g.by_token, g.n);
+    if (a < 0 || a >= g.n) return;  // uniform
+    const int real = (g.R + 15) / 16;  // blocks of 16 that hold ranks
+    for (int t = t0; t < t1; t += kScan) {
+        __syncthreads();  // the list before has been used
+        const int count = tokens_of(g.aid, t, min(kScan, t1 - t), a, g.n, lds.list, &lds.count);
+        for (int at = 0; at < count; at += 32)
+            for (int rb = 0; rb < real; rb += 2) {
+                const int cols = rb + 2 < real ? 32 : g.Rp - rb * 16;
+                if (rb + 1 < real) shrink_tiles<F32, 2>(g, lds, a, rb, cols, at, min(32, count - at));
+                else shrink_tiles<F32, 1>(g, lds, a, rb, cols, at, min(32, count - at));
+            }
+    }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void shrink_kernel(ShrinkArgs g)
+{
+    __shared__ ShrinkLds lds;
+    shrink_body<F32>(g, lds, blockIdx.y, blockIdx.x);
 }
 
 // ---- Y = X W + U B -----------------------------------------------------------------------------------
 struct ProjectArgs {
     const char *X, *Wp, *Bp, *U;
     char* Y;
-    float* part;         // [splits][T][N] where the reduction is split
+    float* part;         // not null: [splits][T][N] parts of X W, which another kernel adds up and the adapters to them
     const int32_t* aid;
     int64_t ldx, ldy;
     int T, K, N, Rp, n;
@@ -116,19 +206,26 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 //   multiplies step t, reads step t + 1's fragments, and copies step t + kStages into the stage of t.
 // The copies are in assembly and nothing else in the loop is a vector memory instruction, so the waits that
 // order them can count: kStages - 2 steps' copies may be in flight at a barrier.
+template <int WM, int WN>
+struct TileLds {
+    static constexpr int kStages = 4, kStep = (WM + WN) * 2048;  // bytes of a step: 2 WM token fragments, then 2 WN of weights
+    __attribute__((aligned(1024))) char ring[kStages * kStep];
+    uint32_t used[kMaxAdapters / 32];
+};
+
 template <bool F32, int WM, int WN>
-__global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel(ProjectArgs g)
+__device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>& shared, int block, int blocks)
 {
     constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
-    constexpr int kStages = 4, kStep = (WM + WN) * 2048;    // bytes of a step: 2 WM token fragments, then 2 WN of weights
+    constexpr int kStages = TileLds<WM, WN>::kStages, kStep = TileLds<WM, WN>::kStep;
     constexpr int kCopies = (WM + WN) / 2;                  // of a wavefront and step
     static_assert(WM % 2 == 0 && WN % 2 == 0, "copies are shared out evenly");
-    __shared__ __attribute__((aligned(1024))) char lds[kStages * kStep];
-    __shared__ uint32_t used[kMaxAdapters / 32];
+    char* const lds = shared.ring;
+    uint32_t* const used = shared.used;
 
     // XCD x (workgroup id mod 8) takes a run of tiles: eight feature tiles of a token tile, then the next token tile.
-    const int all = g.tiles_m * g.tiles_n * g.splits, per = gridDim.x / 8;
-    int tile = blockIdx.x % 8 * per + blockIdx.x / 8;
+    const int all = g.tiles_m * g.tiles_n * g.splits, per = blocks / 8;
+    int tile = block % 8 * per + block / 8;
     if (tile >= all) return;  // uniform
     const int split = tile % g.splits;
     tile /= g.splits;
@@ -183,7 +280,7 @@ __global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel
         frag[set][i] = *(const u32x4*)(lds + stage * kStep + at * 1024 + lane * 16);
     };
     auto arrived = [](const u32x4& f) { asm volatile("" ::"v"(f)); };
-    if (g.n) {  // adapters of the tile's tokens
+    if (g.n && !g.part) {  // adapters of the tile's tokens
         if (tid < kMaxAdapters / 32) used[tid] = 0;
         __syncthreads();
         for (int t = t0 + tid; t < min(t0 + 32 * WM, g.T); t += 256) {
@@ -226,7 +323,7 @@ __global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");  // no copy is on its way when the workgroup ends
 
     // adapters that the tile's tokens use, one by one; tokens of other adapters with zeros
-    if (g.n && split == 0) {
+    if (g.n && !g.part) {
         const int rs = g.Rp * kEsz / 64;
         int mine[WM];
         const char* u[WM];
@@ -272,7 +369,7 @@ __global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel
 #pragma unroll
     for (int j = 0; j < WM; ++j) {
         const int t = t0 + (wm * WM + j) * 16 + lr;
-        if (g.splits > 1) {
+        if (g.part) {
             float* y = g.part + ((int64_t)split * g.T + t) * g.N + (f0 + wn * WN) * 16 + lg * 4;
             if (t < g.T)
 #pragma unroll
@@ -296,35 +393,87 @@ __global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel
     }
 }
 
-// Y = the sum of the splits' parts, in their order.
-template <bool F32>
-__global__ __launch_bounds__(256) void project_sum_kernel(const float* __restrict__ part, char* __restrict__ Y, int64_t ldy, int T, int N,
-                                                          int splits)
+template <bool F32, int WM, int WN>
+__global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel(ProjectArgs g)
 {
-    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (int64_t)T * N;
-    if (id >= all) return;
-    f32x4 v = *(const f32x4*)(part + id);
-    for (int s = 1; s < splits; ++s) v += *(const f32x4*)(part + s * all + id);
-    const int64_t at = id / N * ldy + id % N;
-    if (F32) *(f32x4*)((float*)Y + at) = v;
-    else *(u32x2*)((uint16_t*)Y + at) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    __shared__ TileLds<WM, WN> lds;
+    tile_body<F32, WM, WN>(g, lds, blockIdx.x, gridDim.x);
 }
 
-// Tile and splits of the reduction.
+// Few tokens: the parts of X W, and U beside them in the same launch.
+template <bool F32, int WM, int WN>
+__global__ __launch_bounds__(256, 2) void project_parts_kernel(ProjectArgs g, ShrinkArgs u, int tiles)
+{
+    __shared__ union {
+        TileLds<WM, WN> tile;
+        ShrinkLds shrink;
+    } lds;
+    if ((int)blockIdx.x < tiles) tile_body<F32, WM, WN>(g, lds.tile, blockIdx.x, tiles);
+    else shrink_body<F32>(u, lds.shrink, blockIdx.x - tiles, 0);
+}
+
+// Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes the tokens of one adapter (or of none) and 256 features,
+// 64 to a wavefront.
+template <bool F32>
+__global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool by_token)
+{
+    constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
+    __shared__ int list[kScan], shared_count;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    const int a = adapter_of(g.aid, 0, g.T, blockIdx.y, by_token, g.n);
+    if (a < 0) return;  // uniform
+    const int count = tokens_of(g.aid, 0, g.T, a, g.n, list, &shared_count);
+    const int nb = (blockIdx.x * 4 + wave) * 4, rs = a < g.n ? g.Rp * kEsz / 64 : 0;
+    const char* b = g.Bp + ((int64_t)a * (g.N / 16) + nb) * rs * 1024 + lane * 16;
+    for (int at = 0; at < count; at += 16) {
+        const int64_t t = list[min(at + lr, count - 1)];
+        const float* part = g.part + t * g.N + nb * 16 + lg * 4;
+        f32x4 acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = *(const f32x4*)(part + i * 16);
+        for (int s = 1; s < g.splits; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += *(const f32x4*)(part + (int64_t)s * g.T * g.N + i * 16);
+        const char* u = g.U + t * kParts * g.Rp * kEsz + lg * 16;
+        for (int s = 0; s < rs; ++s) {
+            u32x4 uf[kParts], wf[4];
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) uf[p] = *(const u32x4*)(u + p * g.Rp * kEsz + s * 64);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) wf[i] = *(const u32x4*)(b + ((int64_t)i * rs + s) * 1024);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] = mma<F32>(wf[i], uf[p], acc[i]);
+        }
+        if (at + lr < count)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                char* y = g.Y + (t * g.ldy + (nb + i) * 16 + lg * 4) * kEsz;
+                if (F32) *(f32x4*)y = acc[i];
+                else *(u32x2*)y = u32x2{pack_bf16(acc[i][0], acc[i][1]), pack_bf16(acc[i][2], acc[i][3])};
+            }
+    }
+}
+
+// Few tokens run in two launches: parts of X W beside U, then their join with U B.  More in two as well: U, then tiles
+// that add U B themselves.
+constexpr int kFewTokens = kScan;
 struct ProjectPlan {
     int wm, wn, splits;
+    bool few;
 };
 static ProjectPlan project_plan(const mmoe_project_shape& s)
 {
     ProjectPlan p;
     auto tiles = [&](int wm, int wn) { return (int64_t)((s.T + 32 * wm - 1) / (32 * wm)) * (s.d_out / (32 * wn)); };
-    if (tiles(8, 8) >= 200) p = {8, 8, 1};
-    else if (s.T > 64) p = {4, 4, 1};
-    else p = {2, 4, 1};
+    if (tiles(8, 8) >= 200) p = {8, 8, 1, false};
+    else if (s.T > 64) p = {4, 4, 1, s.T <= kFewTokens};
+    else p = {2, 4, 1, true};
     const int64_t n = tiles(p.wm, p.wn);
-    const int most = s.d_in / 512 > 0 ? s.d_in / 512 : 1;
-    if (p.wm < 8)
-        while (p.splits < most && n * p.splits < 256) ++p.splits;
+    const int most = s.d_in / 256;
+    if (p.few)
+        while (p.splits < most && n * (p.splits + 1) <= 256) ++p.splits;
     return p;
 }
 
@@ -333,7 +482,7 @@ static size_t u_bytes(const mmoe_project_shape& s) { return s.n_adapters ? align
 static size_t part_bytes(const mmoe_project_shape& s)
 {
     const ProjectPlan p = project_plan(s);
-    return p.splits > 1 ? align256((size_t)p.splits * s.T * s.d_out * 4) : 0;
+    return p.few ? align256((size_t)p.splits * s.T * s.d_out * 4) : 0;
 }
 
 // What a call of this shape uses.
@@ -348,7 +497,7 @@ size_t project_ws_bytes(const mmoe_project_shape& s)
         q.T = T < s.T ? T : s.T;
         const size_t b = part_bytes(q);
         if (b > most) most = b;
-        if (T >= s.T || T >= 16384) break;  // from there on there are 256 tiles of 128 tokens for any d_out
+        if (T >= s.T || T >= kFewTokens) break;
     }
     return u_bytes(s) + most;
 }
@@ -359,20 +508,31 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
 {
     const int64_t ldx = s.ldx ? s.ldx : s.d_in, ldy = s.ldy ? s.ldy : s.d_out;
     const int n = s.n_adapters, rp = n ? padded_rank(s) : 0;
-    if (n)
-        hipLaunchKernelGGL(shrink_kernel<F32>, dim3((s.T + 15) / 16), dim3(256), 0, st, (const char*)X, ldx, aid, (const char*)Ap, scale,
-                           (char*)ws, s.T, s.d_in, rp, n);
     const ProjectPlan p = project_plan(s);
-    ProjectArgs g = {(const char*)X, (const char*)Wp, (const char*)Bp, (const char*)ws, (char*)Y, (float*)((char*)ws + u_bytes(s)), aid, ldx, ldy,
-                     s.T, s.d_in, s.d_out, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
-    const dim3 grid((g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8), block(256);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
+    ProjectArgs g = {(const char*)X, (const char*)Wp, (const char*)Bp, (const char*)ws, (char*)Y, p.few ? (float*)((char*)ws + u_bytes(s)) : nullptr, aid,
+                     ldx, ldy, s.T, s.d_in, s.d_out, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
+    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, false};
+    const int tiles = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
+    const dim3 block(256);
+    if (p.few) {
+        const bool by_token = n + 1 > s.T;
+        u.by_token = by_token;
+        const dim3 grid(tiles + (n ? by_token ? s.T : n : 0));
+        if (p.wm == 4) hipLaunchKernelGGL((project_parts_kernel<F32, 4, 4>), grid, block, 0, st, g, u, tiles);
+        else hipLaunchKernelGGL((project_parts_kernel<F32, 2, 4>), grid, block, 0, st, g, u, tiles);
+        hipLaunchKernelGGL(project_join_kernel<F32>, dim3(s.d_out / 256, by_token ? s.T : n + 1), block, 0, st, g, by_token);
+        return;
+    }
+    if (n) {
+        // about 512 workgroups: chunks of 32 tokens and more
+        const int chunks = n >= 512 ? 1 : 512 / n;
+        u.chunk = (s.T + chunks - 1) / chunks;
+        if (u.chunk < 32) u.chunk = 32;
+        hipLaunchKernelGGL(shrink_kernel<F32>, dim3((s.T + u.chunk - 1) / u.chunk, n), block, 0, st, u);
+    }
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles), block, 0, st, g); };
     if (p.wm == 8) go(project_tile_kernel<F32, 8, 8>);
-    else if (p.wm == 4) go(project_tile_kernel<F32, 4, 4>);
-    else go(project_tile_kernel<F32, 2, 4>);
-    if (p.splits > 1)
-        hipLaunchKernelGGL(project_sum_kernel<F32>, dim3((unsigned)(((int64_t)s.T * s.d_out / 4 + 255) / 256)), block, 0, st, g.part, (char*)Y, ldy,
-                           s.T, s.d_out, p.splits);
+    else go(project_tile_kernel<F32, 4, 4>);
 }
 
 int launch_project(const mmoe_project_shape& s, const void* X, const int32_t* aid, const void* Wp, const void* Ap, const void* Bp,
