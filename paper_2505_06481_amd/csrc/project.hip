@@ -208,7 +208,9 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 // order them can count: kStages - 2 steps' copies may be in flight at a barrier.
 template <int WM, int WN>
 struct TileLds {
-    static constexpr int kStages = 4, kStep = (WM + WN) * 2048;  // bytes of a step: 2 WM token fragments, then 2 WN of weights
+    static constexpr int kStep = (WM + WN) * 2048;  // bytes of a step: 2 WM token fragments, then 2 WN of weights
+    // steps in the ring: small tiles have as many bytes in flight as large ones; 128 x 256 leaves room for two workgroups
+    static constexpr int kStages = WM == 2 ? 8 : WM == 4 && WN == 8 ? 3 : 4;
     __attribute__((aligned(1024))) char ring[kStages * kStep];
     uint32_t used[kMaxAdapters / 32];
 };
@@ -250,12 +252,12 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
     const char* w_base = g.Wp + ((int64_t)(f0 + wave * (WN / 2)) * slices + k0) * 1024;
     const uint32_t w_off = lane * 16;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr)lds;
-    auto copy = [&](int step, int stage, int i) {
+    auto copy = [&](int step, int stage, int i) {  // stage: byte offset in the ring
         const int at = min(step, last);
         const bool tokens = i < WM / 2;
         const char* base = tokens ? x_base + (int64_t)at * 64 : w_base + ((int64_t)(i - WM / 2) * slices + at) * 1024;
         const uint32_t off = tokens ? x_off[tokens ? i : 0] : w_off;
-        const uint32_t dst = lds0 + stage * kStep + (tokens ? wave * (WM / 2) + i : 2 * WM + wave * (WN / 2) + i - WM / 2) * 1024;
+        const uint32_t dst = lds0 + stage + (tokens ? wave * (WM / 2) + i : 2 * WM + wave * (WN / 2) + i - WM / 2) * 1024;
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(dst) : "m0", "memory");
     };
 
@@ -275,9 +277,10 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
     };
 
     u32x4 frag[2][WM + WN];
+    const char* const lds_x = lds + wm * WM * 1024 + lane * 16;
+    const char* const lds_w = lds + (2 * WM + wn * WN) * 1024 + lane * 16;
     auto read = [&](int set, int stage, int i) {
-        const int at = i < WM ? wm * WM + i : 2 * WM + wn * WN + i - WM;
-        frag[set][i] = *(const u32x4*)(lds + stage * kStep + at * 1024 + lane * 16);
+        frag[set][i] = *(const u32x4*)(i < WM ? lds_x + stage + i * 1024 : lds_w + stage + (i - WM) * 1024);
     };
     auto arrived = [](const u32x4& f) { asm volatile("" ::"v"(f)); };
     if (g.n && !g.part) {  // adapters of the tile's tokens
@@ -293,14 +296,16 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
 #pragma unroll
     for (int s = 0; s < kStages; ++s)
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy(s, s, i);
+        for (int i = 0; i < kCopies; ++i) copy(s, s * kStep, i);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 1) * kCopies) : "memory");
 #pragma unroll
     for (int i = 0; i < WM + WN; ++i) read(0, 0, i);
 
-    for (int t = 0; t <= last; t += kStages) {
-        each<kStages>([&](auto uc) {
-            constexpr int u = decltype(uc)::value, set = u & 1, kUnits = WM * WN, kReads = WM + WN;
+    int stage = 0;
+    for (int t = 0; t <= last; t += 2) {  // (an even number of steps: eight slices to 256 k)
+        each<2>([&](auto uc) {
+            const int next = stage == (kStages - 1) * kStep ? 0 : stage + kStep;
+            constexpr int u = decltype(uc)::value, set = u, kUnits = WM * WN, kReads = WM + WN;
             each<kReads>([&](auto i) { arrived(frag[set][decltype(i)::value]); });
             asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kCopies) : "memory");
             __builtin_amdgcn_sched_barrier(0);
@@ -310,51 +315,65 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
                 // reads in the first half, copies in the second
                 each<kReads>([&](auto ic) {
                     constexpr int i = decltype(ic)::value;
-                    if constexpr (i * (kUnits / 2) / kReads == x) read(set ^ 1, (u + 1) % kStages, i);
+                    if constexpr (i * (kUnits / 2) / kReads == x) read(set ^ 1, next, i);
                 });
                 each<kCopies>([&](auto ic) {
                     constexpr int i = decltype(ic)::value;
-                    if constexpr (kUnits / 2 + i * (kUnits / 2) / kCopies == x) copy(t + u + kStages, u, i);
+                    if constexpr (kUnits / 2 + i * (kUnits / 2) / kCopies == x) copy(t + u + kStages, stage, i);
                 });
                 __builtin_amdgcn_sched_barrier(0);
             });
+            stage = next;
         });
     }
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");  // no copy is on its way when the workgroup ends
 
-    // adapters that the tile's tokens use, one by one; tokens of other adapters with zeros
+    // Adapters that the tile's tokens use, one by one: tokens of other adapters with zeros, fragments without any not at all.  A token's
+    // U is its own adapter's, read once; the weights of the next adapter are on their way while this one's are multiplied.
     if (g.n && !g.part) {
         const int rs = g.Rp * kEsz / 64;
         int mine[WM];
-        const char* u[WM];
 #pragma unroll
-        for (int j = 0; j < WM; ++j) {
-            const int t = min(t0 + (wm * WM + j) * 16 + lr, g.T - 1);
-            mine[j] = g.aid[t];
-            u[j] = g.U + (int64_t)t * kParts * g.Rp * kEsz + lg * 16;
-        }
-        for (int word = 0; word < (g.n + 31) / 32; ++word) {
-            uint32_t bits = __builtin_amdgcn_readfirstlane(used[word]);
-            while (bits) {
+        for (int j = 0; j < WM; ++j) mine[j] = g.aid[min(t0 + (wm * WM + j) * 16 + lr, g.T - 1)];
+        for (int s = 0; s < rs; ++s) {
+            u32x4 uf[WM][kParts], wf[WN], ahead[WN];
+#pragma unroll
+            for (int j = 0; j < WM; ++j)
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    uf[j][p] = *(const u32x4*)(g.U + ((int64_t)min(t0 + (wm * WM + j) * 16 + lr, g.T - 1) * kParts + p) * g.Rp * kEsz + s * 64 + lg * 16);
+            int word = 0;
+            uint32_t bits = __builtin_amdgcn_readfirstlane(used[0]);
+            auto next = [&]() {  // of the tile's adapters; -1: no more
+                while (!bits && ++word < (g.n + 31) / 32) bits = __builtin_amdgcn_readfirstlane(used[word]);
+                if (!bits) return -1;
                 const int a = word * 32 + __ffs(bits) - 1;
                 bits &= bits - 1;
-                const char* b = g.Bp + ((int64_t)a * (g.N / 16) + f0 + wn * WN) * rs * 1024 + lane * 16;
-                for (int s = 0; s < rs; ++s) {
-                    u32x4 wf[WN], uf[WM][kParts];
+                return a;
+            };
+            auto fetch = [&](int a) {
+                const char* b = g.Bp + (((int64_t)max(a, 0) * (g.N / 16) + f0 + wn * WN) * rs + s) * 1024 + lane * 16;
+                each<WN>([&](auto i) { ahead[decltype(i)::value] = *(const u32x4*)(b + (int64_t)decltype(i)::value * rs * 1024); });
+            };
+            int a = next();
+            if (a >= 0) fetch(a);
+            while (a >= 0) {
+                each<WN>([&](auto i) { wf[decltype(i)::value] = ahead[decltype(i)::value]; });
+                const int then = next();
+                fetch(then);
+                each<WM>([&](auto jc) {
+                    constexpr int j = decltype(jc)::value;
+                    if (!__any(mine[j] == a)) return;  // uniform
+                    u32x4 u[kParts];
 #pragma unroll
-                    for (int i = 0; i < WN; ++i) wf[i] = *(const u32x4*)(b + ((int64_t)i * rs + s) * 1024);
-#pragma unroll
-                    for (int j = 0; j < WM; ++j)
-#pragma unroll
-                        for (int p = 0; p < kParts; ++p)
-                            uf[j][p] = mine[j] == a ? *(const u32x4*)(u[j] + p * g.Rp * kEsz + s * 64) : u32x4{0, 0, 0, 0};
-                    // a vector instruction's result needs its time before a matrix instruction that the compiler does not see reads it
-                    asm volatile("s_nop 7" ::: "memory");
-                    each<kParts * WM * WN>([&](auto xc) {
-                        constexpr int x = decltype(xc)::value, j = x % WM, i = x / WM % WN, p = x / (WM * WN);
-                        multiply(acc[j][i], wf[i], uf[j][p]);
+                    for (int p = 0; p < kParts; ++p) u[p] = mine[j] == a ? uf[j][p] : u32x4{0, 0, 0, 0};
+                    // (by the builtin: between branches the compiler has to know which registers a matrix instruction still writes)
+                    each<kParts * WN>([&](auto xc) {
+                        constexpr int i = decltype(xc)::value % WN, p = decltype(xc)::value / WN;
+                        acc[j][i] = mma<F32>(wf[i], u[p], acc[j][i]);
                     });
-                }
+                });
+                a = then;
             }
         }
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -394,7 +413,7 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
 }
 
 template <bool F32, int WM, int WN>
-__global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel(ProjectArgs g)
+__global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_tile_kernel(ProjectArgs g)
 {
     __shared__ TileLds<WM, WN> lds;
     tile_body<F32, WM, WN>(g, lds, blockIdx.x, gridDim.x);
@@ -402,7 +421,7 @@ __global__ __launch_bounds__(256, WM * WN > 16 ? 1 : 2) void project_tile_kernel
 
 // Few tokens: the parts of X W, and U beside them in the same launch.
 template <bool F32, int WM, int WN>
-__global__ __launch_bounds__(256, 2) void project_parts_kernel(ProjectArgs g, ShrinkArgs u, int tiles)
+__global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_parts_kernel(ProjectArgs g, ShrinkArgs u, int tiles)
 {
     __shared__ union {
         TileLds<WM, WN> tile;
@@ -412,8 +431,8 @@ __global__ __launch_bounds__(256, 2) void project_parts_kernel(ProjectArgs g, Sh
     else shrink_body<F32>(u, lds.shrink, blockIdx.x - tiles, 0);
 }
 
-// Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes the tokens of one adapter (or of none) and 256 features,
-// 64 to a wavefront.
+// Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes tokens of one adapter (or of none), 16 of every
+// gridDim.z times 16, and 256 features, 64 to a wavefront.
 template <bool F32>
 __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool by_token)
 {
@@ -425,7 +444,7 @@ __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool b
     const int count = tokens_of(g.aid, 0, g.T, a, g.n, list, &shared_count);
     const int nb = (blockIdx.x * 4 + wave) * 4, rs = a < g.n ? g.Rp * kEsz / 64 : 0;
     const char* b = g.Bp + ((int64_t)a * (g.N / 16) + nb) * rs * 1024 + lane * 16;
-    for (int at = 0; at < count; at += 16) {
+    for (int at = blockIdx.z * 16; at < count; at += gridDim.z * 16) {
         const int64_t t = list[min(at + lr, count - 1)];
         const float* part = g.part + t * g.N + nb * 16 + lg * 4;
         f32x4 acc[4];
@@ -463,18 +482,38 @@ struct ProjectPlan {
     int wm, wn, splits;
     bool few;
 };
+
+// The plan with the least estimated time, in cycles.  A step of a tile, alone on its compute unit and beside a second one, as
+// measured with 4096 k (8192 x 8192 x 8192 in 256 x 256 tiles reaches 1.31 PFLOP/s); fp32 is bound by its matrix rate.
 static ProjectPlan project_plan(const mmoe_project_shape& s)
 {
-    ProjectPlan p;
-    auto tiles = [&](int wm, int wn) { return (int64_t)((s.T + 32 * wm - 1) / (32 * wm)) * (s.d_out / (32 * wn)); };
-    if (tiles(8, 8) >= 200) p = {8, 8, 1, false};
-    else if (s.T > 64) p = {4, 4, 1, s.T <= kFewTokens};
-    else p = {2, 4, 1, true};
-    const int64_t n = tiles(p.wm, p.wn);
-    const int most = s.d_in / 256;
-    if (p.few)
-        while (p.splits < most && n * (p.splits + 1) <= 256) ++p.splits;
-    return p;
+    struct Tile {
+        int wm, wn;
+        double alone, two, ends;  // cycles of a step; of one of each of two; of a tile's beginning and end
+    };
+    static const Tile tiles[] = {{8, 8, 1450.0, 0.0, 25000.0}, {4, 8, 900.0, 1800.0, 15000.0}, {4, 4, 680.0, 1430.0, 6000.0}, {2, 4, 440.0, 0.0, 4000.0}};
+    constexpr double kLaunch = 7000.0, kBytes = 1200.0;  // a launch more; bytes of parts a cycle
+    const bool f32 = s.dtype == MMOE_F32;
+    const int slices = s.d_in / (f32 ? 16 : 32);
+    const int T = (s.T + 31) / 32 * 32, most = s.T > kFewTokens ? 0 : s.d_in / 256 < 16 ? s.d_in / 256 : 16;
+    ProjectPlan best = {8, 8, 1, false};
+    double least = 1e30;
+    for (const Tile& t : tiles) {
+        const int64_t n = (int64_t)((T + 32 * t.wm - 1) / (32 * t.wm)) * (s.d_out / (32 * t.wn));
+        const double matrix = f32 ? t.wm * t.wn * 135.0 : 0.0;
+        for (int splits = 0; splits <= most; ++splits) {  // 0: not in parts
+            // beside the parts run the workgroups that make U
+            const int64_t wgs = splits ? n * splits + (s.n_adapters < T ? s.n_adapters : T) : n, room = t.two > 0.0 ? 512 : 256, full = wgs / room, rest = wgs % room;
+            const double steps = (double)slices / (splits ? splits : 1);
+            const double alone = (t.alone > matrix ? t.alone : matrix) * steps + t.ends;
+            const double two = (t.two > 2.0 * matrix ? t.two : 2.0 * matrix) * steps + t.ends;
+            double time = full * (room == 512 ? two : alone) + (rest > 256 ? two : rest ? alone : 0.0);
+            if (splits) time += kLaunch + (2.0 * splits + 1.0) * T * s.d_out * 4.0 / kBytes;
+            else if (s.n_adapters) time += 2.5 * kLaunch + 700.0 * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
+            if (time < least) least = time, best = {t.wm, t.wn, splits ? splits : 1, splits > 0};
+        }
+    }
+    return best;
 }
 
 static size_t u_bytes(const mmoe_project_shape& s) { return s.n_adapters ? align256((size_t)s.T * padded_rank(s) * 4) : 0; }  // fp32 or two bf16 parts
@@ -488,11 +527,11 @@ static size_t part_bytes(const mmoe_project_shape& s)
 // What a call of this shape uses.
 size_t project_need(const mmoe_project_shape& s) { return u_bytes(s) + part_bytes(s); }
 
-// The most that one of up to this many tokens does.
+// The most that one of up to this many tokens does: parts are of kFewTokens tokens at most and of 256 k at least.
 size_t project_ws_bytes(const mmoe_project_shape& s)
 {
     size_t most = 0;
-    for (int T = 64;; T += 64) {  // the plan is the same within 64 tokens
+    for (int T = 32;; T += 32) {  // the plan is the same within 32 tokens
         mmoe_project_shape q = s;
         q.T = T < s.T ? T : s.T;
         const size_t b = part_bytes(q);
@@ -518,9 +557,14 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
         const bool by_token = n + 1 > s.T;
         u.by_token = by_token;
         const dim3 grid(tiles + (n ? by_token ? s.T : n : 0));
-        if (p.wm == 4) hipLaunchKernelGGL((project_parts_kernel<F32, 4, 4>), grid, block, 0, st, g, u, tiles);
-        else hipLaunchKernelGGL((project_parts_kernel<F32, 2, 4>), grid, block, 0, st, g, u, tiles);
-        hipLaunchKernelGGL(project_join_kernel<F32>, dim3(s.d_out / 256, by_token ? s.T : n + 1), block, 0, st, g, by_token);
+        auto parts = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g, u, tiles); };
+        if (p.wm == 8) parts(project_parts_kernel<F32, 8, 8>);
+        else if (p.wn == 8) parts(project_parts_kernel<F32, 4, 8>);
+        else if (p.wm == 4) parts(project_parts_kernel<F32, 4, 4>);
+        else parts(project_parts_kernel<F32, 2, 4>);
+        // as many workgroups to an adapter as its even share of the tokens has sixteens
+        const int groups = by_token ? s.T : n + 1, share = (s.T + 16 * groups - 1) / (16 * groups);
+        hipLaunchKernelGGL(project_join_kernel<F32>, dim3(s.d_out / 256, groups, share), block, 0, st, g, by_token);
         return;
     }
     if (n) {
@@ -532,7 +576,9 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
     }
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles), block, 0, st, g); };
     if (p.wm == 8) go(project_tile_kernel<F32, 8, 8>);
-    else go(project_tile_kernel<F32, 4, 4>);
+    else if (p.wn == 8) go(project_tile_kernel<F32, 4, 8>);
+    else if (p.wm == 4) go(project_tile_kernel<F32, 4, 4>);
+    else go(project_tile_kernel<F32, 2, 4>);
 }
 
 int launch_project(const mmoe_project_shape& s, const void* X, const int32_t* aid, const void* Wp, const void* Ap, const void* Bp,
