@@ -8,12 +8,11 @@ from __future__ import annotations
 
 import ctypes
 import functools
-from typing import NamedTuple, Optional
 
 import torch
 
 from . import mmoe
-from .mmoe import _check, _ptr, _stream, lib
+from .mmoe import MmoeError, _ptr, _stream, lib
 
 HALVES, NEIGHBOURS = 0, 1
 PLAIN, INT8, FP8 = 0, 1, 2
@@ -22,6 +21,11 @@ _LAYOUTS = {"halves": HALVES, "neighbours": NEIGHBOURS}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
 _FORMATS = {"plain": PLAIN, "int8": INT8, "fp8": FP8}
 _I32, _F32 = torch.int32, torch.float32
+
+
+def _check(rc, where):
+    if rc:
+        raise MmoeError(rc, where)
 
 
 def _code(value, names):
@@ -60,12 +64,31 @@ class AttendShape(ctypes.Structure):
                 + _fields(("q_token", "q_head", "o_token", "o_head"), ctypes.c_int64))
 
 
-class Cache(NamedTuple):
-    """Pages of keys and values (bytes in the layout of include/mmoe.h) and their scales (None for plain pages)."""
-    k: torch.Tensor
-    v: torch.Tensor
-    k_scale: Optional[torch.Tensor]
-    v_scale: Optional[torch.Tensor]
+class Cache:
+    """Pages of keys and values (bytes in the layout of include/mmoe.h) and their scales (None for plain pages), on the GPU.
+    Iterates over (k, v, k_scale, v_scale).  The tensors are looked at once: they stay what and where they are."""
+    __slots__ = ("_tensors", "_pointers", "_bytes")
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        self._tensors = (k, v, k_scale, v_scale)
+        if (k_scale is None) != (v_scale is None):
+            raise ValueError("k_scale and v_scale go together")
+        self._pointers = _CachePointers(_ptr(k, torch.uint8, None, "k"), _ptr(v, torch.uint8, None, "v"), _ptr(k_scale, _F32, None, "k_scale"),
+                                        _ptr(v_scale, _F32, None, "v_scale"))
+        self._bytes = (min(k.numel(), v.numel()), 0 if k_scale is None else 4 * min(k_scale.numel(), v_scale.numel()))
+
+    k, v, k_scale, v_scale = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
+
+    def __iter__(self):
+        return iter(self._tensors)
+
+    def address(self, shape):
+        """Address of the pointers, for a shape whose pages they have room for."""
+        rows = shape.n_pages * shape.kv_heads * PAGE_TOKENS
+        kept = rows * shape.head_dim * (1 if shape.format else 4 if shape.dtype == mmoe.F32 else 2)
+        if self._bytes[0] < kept or (shape.format and self._bytes[1] < 4 * rows):
+            raise ValueError(f"the cache holds {self._bytes} bytes, the shape needs {kept} and {4 * rows if shape.format else 0}")
+        return ctypes.addressof(self._pointers)
 
 
 @functools.lru_cache(maxsize=None)
@@ -96,6 +119,10 @@ def _dtype(dtype):
 
 def _heads_view(t, dtype, T, heads, head_dim, name):
     """Pointer and (token, head) strides of a [T, heads, head_dim] tensor or view whose heads are contiguous."""
+    if t.is_cuda and t.dtype is dtype and t.shape == (T, heads, head_dim):
+        a, b, c = t.stride()
+        if c == 1 and b >= head_dim and a >= b * heads:
+            return t.data_ptr(), a, b
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
     if t.dtype != dtype:
@@ -151,6 +178,8 @@ def pack_adapters(shape: ProjectShape, A, B):
 
 def _rows_ptr(t, dtype, rows, cols, ld, name):
     """Pointer of [rows, cols] with rows ``ld`` apart (0: dense)."""
+    if t.is_cuda and t.dtype is dtype and t.shape == (rows, cols) and t.stride() == (ld or cols, 1):
+        return t.data_ptr()
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
     if t.dtype != dtype:
@@ -167,7 +196,7 @@ def project(shape: ProjectShape, X, aid, Wp, Ap, Bp, scale, ws, Y=None):
     dt, n = mmoe._TORCH_DT[shape.dtype], shape.n_adapters
     T, K, N = shape.T, shape.d_in, shape.d_out
     if Y is None:
-        Y = torch.empty((T, N), dtype=dt, device=X.device) if not shape.ldy else \
+        Y = X.new_empty((T, N)) if not shape.ldy else \
             torch.empty((T, shape.ldy), dtype=dt, device=X.device)[:, :N]
     rank = (shape.rank + 31) // 32 * 32 if dt == torch.bfloat16 else (shape.rank + 15) // 16 * 16
     rc = _entry("mmoe_project")(
@@ -198,10 +227,11 @@ def rotary(shape: RotaryShape, X, pos, steps, Y=None):
     dt = mmoe._TORCH_DT[shape.dtype]
     T, H, D = shape.T, shape.heads, shape.head_dim
     if Y is None:
-        Y = torch.empty((T, H, D), dtype=dt, device=X.device)
-    x, shape.x_token, shape.x_head = _heads_view(X, dt, T, H, D, "X")
-    y, shape.y_token, shape.y_head = _heads_view(Y, dt, T, H, D, "Y")
-    rc = _entry("mmoe_rotary")(ctypes.addressof(shape), x, _ptr(pos, _I32, T, "pos"), _ptr(steps, torch.int64, shape.rot // 2, "steps"), y,
+        Y = X.new_empty((T, H, D))
+    x, xt, xh = _heads_view(X, dt, T, H, D, "X")
+    y, yt, yh = _heads_view(Y, dt, T, H, D, "Y")
+    call = RotaryShape(T, H, D, shape.rot, shape.layout, shape.dtype, shape.transpose, shape.magnitude, xt, xh, yt, yh)
+    rc = _entry("mmoe_rotary")(ctypes.addressof(call), x, _ptr(pos, _I32, T, "pos"), _ptr(steps, torch.int64, shape.rot // 2, "steps"), y,
                                _stream())
     _check(rc, "mmoe_rotary")
     return Y
@@ -228,13 +258,6 @@ def alloc_cache(shape: CacheShape, device="cuda") -> Cache:
     return Cache(k, v, ks, vs)
 
 
-def _cache_pointers(shape: CacheShape, cache: Cache):
-    n = shape.n_pages * shape.kv_heads * PAGE_TOKENS
-    kept = n * shape.head_dim * (1 if shape.format else 4 if shape.dtype == mmoe.F32 else 2)
-    scales = (_ptr(cache.k_scale, _F32, n, "k_scale"), _ptr(cache.v_scale, _F32, n, "v_scale")) if shape.format else (None, None)
-    return _CachePointers(_ptr(cache.k, torch.uint8, kept, "cache.k"), _ptr(cache.v, torch.uint8, kept, "cache.v"), *scales)
-
-
 def cache_append(shape: CacheShape, K, V, places, cache: Cache, rotary=None):
     """Writes K, V [T, kv_heads, head_dim] (views are fine) to the places of their tokens.  ``rotary``: (RotaryShape, steps,
     pos) turns the keys first."""
@@ -244,13 +267,13 @@ def cache_append(shape: CacheShape, K, V, places, cache: Cache, rotary=None):
         return
     k, kt, kh = _heads_view(K, dt, T, H, D, "K")
     v, vt, vh = _heads_view(V, dt, T, H, D, "V")
-    rows, pointers = _CacheRows(T, kt, kh, vt, vh), _cache_pointers(shape, cache)
+    rows = _CacheRows(T, kt, kh, vt, vh)
     turn = steps = pos = None
     if rotary is not None:
         spec, steps, pos = rotary
         turn, steps, pos = ctypes.addressof(spec), _ptr(steps, torch.int64, spec.rot // 2, "steps"), _ptr(pos, _I32, T, "pos")
     rc = _entry("mmoe_cache_append")(ctypes.addressof(shape), ctypes.addressof(rows), k, v, _ptr(places, _I32, T, "places"), turn, pos, steps,
-                                     ctypes.addressof(pointers), _stream())
+                                     cache.address(shape), _stream())
     _check(rc, "mmoe_cache_append")
 
 
@@ -264,8 +287,7 @@ def cache_read(shape: CacheShape, cache: Cache, places, K=None, V=None):
         V = torch.empty((R, H, D), dtype=dt, device=places.device)
     if R == 0:
         return K, V
-    pointers = _cache_pointers(shape, cache)
-    rc = _entry("mmoe_cache_read")(ctypes.addressof(shape), ctypes.addressof(pointers), R, _ptr(places, _I32, R, "places"),
+    rc = _entry("mmoe_cache_read")(ctypes.addressof(shape), cache.address(shape), R, _ptr(places, _I32, R, "places"),
                                    _ptr(K, dt, R * H * D, "K"), _ptr(V, dt, R * H * D, "V"), _stream())
     _check(rc, "mmoe_cache_read")
     return K, V
@@ -298,15 +320,16 @@ def attend(shape: AttendShape, Q, starts, ctx, tree, pages, cache: Cache, ws, ou
     dt = mmoe._TORCH_DT[c.dtype]
     T, H, D, B = shape.T, shape.heads, c.head_dim, shape.n_requests
     if out is None:
-        out = torch.empty((T, H, D), dtype=dt, device=Q.device)
+        out = Q.new_empty((T, H, D))
     if lse is None:
         lse = torch.empty((T, H), dtype=_F32, device=Q.device)
-    q, shape.q_token, shape.q_head = _heads_view(Q, dt, T, H, D, "Q")
-    o, shape.o_token, shape.o_head = _heads_view(out, dt, T, H, D, "out")
-    pointers = _cache_pointers(c, cache)
-    rc = _entry("mmoe_attend")(ctypes.addressof(shape), q, _ptr(starts, _I32, B + 1, "starts"), _ptr(ctx, _I32, B, "ctx"),
+    q, qt, qh = _heads_view(Q, dt, T, H, D, "Q")
+    o, ot, oh = _heads_view(out, dt, T, H, D, "out")
+    call = AttendShape.from_buffer_copy(shape)
+    call.q_token, call.q_head, call.o_token, call.o_head = qt, qh, ot, oh
+    rc = _entry("mmoe_attend")(ctypes.addressof(call), q, _ptr(starts, _I32, B + 1, "starts"), _ptr(ctx, _I32, B, "ctx"),
                                _ptr(tree, torch.int64, T * shape.mask_words, "tree"), _ptr(pages, _I32, B * shape.max_pages, "pages"),
-                               ctypes.addressof(pointers), o, _ptr(lse, _F32, T * H, "lse"), _ptr(ws, torch.uint8, None, "ws"),
+                               cache.address(c), o, _ptr(lse, _F32, T * H, "lse"), _ptr(ws, torch.uint8, None, "ws"),
                                ws.numel(), _stream())
     _check(rc, "mmoe_attend")
     return out, lse
