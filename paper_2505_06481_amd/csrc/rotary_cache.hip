@@ -180,28 +180,19 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
     const int U = g.D / 16, nthreads = 2 * kTok * U, tid = threadIdx.x;
     char* codes = lds;                                      // [kTok][D] of V
     float* amax = (float*)(lds + kTok * g.D * P::kBytes);   // [2][kTok][U]
-    __shared__ int place[kTok], run[kTok];
+    __shared__ int place[kTok];
     const int t0 = blockIdx.x * kTok, h = blockIdx.y;
-    if (tid < kTok) {
-        const int p = t0 + tid < g.T ? g.places[t0 + tid] : -1;
-        place[tid] = p >= 0 && p < g.n_places ? p : -1;
-    }
-    __syncthreads();
-    if (tid < kTok) {  // 4: first of four consecutive places from a multiple of four on; 0: one of the others of such a run; 1: alone
-        const int p = place[tid], lead = tid - (p & 3);
-        bool whole = p >= 0 && lead >= 0 && lead + 3 < kTok;
-        for (int i = 0; i < 4 && whole; ++i) whole = place[lead + i] == (p & ~3) + i;
-        run[tid] = p < 0 ? 0 : !whole ? 1 : (p & 3) == 0 ? 4 : 0;
-    }
     const int which = tid / (kTok * U), tok = tid / U % kTok, u = tid % U;  // which: 0 keys, 1 values
     const int t = min(t0 + tok, g.T - 1);
-    const int p = place[tok];
     const char* src = which ? g.V + (t * g.vt + h * g.vh) * kEsz : g.K + (t * g.kt + h * g.kh) * kEsz;
     const bool turns = ROTATE && which == 0 && u < g.rot / 16;
     const UnitPlace at = ROTATE == 1 && which == 0 ? unit_place<true>(u, g.rot) : unit_place<false>(u, g.rot);
     float x[16];
     load8<F32>(src + at.a * kEsz, x);
     load8<F32>(src + at.b * kEsz, x + 8);
+    int p = t0 + tok < g.T ? g.places[t] : -1;
+    if (p >= g.n_places) p = -1;
+    if (u == 0 && which == 0) place[tok] = p;
     if (turns) {
         float c[8], s[8];
         turn_of(g.steps + 8 * u, g.pos[t], g.m, g.sign, c, s);
@@ -263,26 +254,38 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
         }
     }
     __syncthreads();
-    for (int i = tid; i < kTok * g.D; i += nthreads) {
-        const int d = i % g.D, k = i / g.D, n = run[k];
-        if (!n) continue;
-        const int q = place[k];
-        char* dst = g.v + (((int64_t)(q / kPage) * g.heads + h) * block + P::v_at(q % kPage, d)) * P::kBytes;
-        const char* from = codes + (k * g.D + d) * P::kBytes;
+    // Four tokens that stand in consecutive places, the first in a multiple of four, are one store for each element; they start at the
+    // first token's distance from such a place.
+    const int shift = -place[0] & 3;
+    for (int i = tid; i < (kTok / 4 + 1) * g.D; i += nthreads) {
+        const int d = i % g.D, first = (i / g.D - 1) * 4 + shift;  // token of the group's first place; the group may begin before the tile
         const int next = g.D * P::kBytes;
-        if constexpr (P::kBytes == 1) {
-            if (n == 4)
-                *(uint32_t*)dst = (uint32_t)(uint8_t)from[0] | (uint32_t)(uint8_t)from[next] << 8 | (uint32_t)(uint8_t)from[2 * next] << 16 |
-                                  (uint32_t)(uint8_t)from[3 * next] << 24;
-            else *dst = *from;
-        } else if constexpr (P::kBytes == 2) {
-            const auto at16 = [&](int j) { return (uint32_t) * (const uint16_t*)(from + j * next); };
-            if (n == 4) *(u32x2*)dst = u32x2{at16(0) | at16(1) << 16, at16(2) | at16(3) << 16};
-            else *(uint16_t*)dst = *(const uint16_t*)from;
+        const char* from = codes + (first * g.D + d) * P::kBytes;
+        auto dst = [&](int q) { return g.v + (((int64_t)(q / kPage) * g.heads + h) * block + P::v_at(q % kPage, d)) * P::kBytes; };
+        bool whole = first >= 0 && first + 3 < kTok && place[first] >= 0 && (place[first] & 3) == 0;
+        if (whole)
+#pragma unroll
+            for (int j = 1; j < 4; ++j) whole = whole && place[first + j] == place[first] + j;
+        if (whole) {
+            char* to = dst(place[first]);
+            if constexpr (P::kBytes == 1) {
+                auto at8 = [&](int j) { return (uint32_t) * (const uint8_t*)(from + j * next); };
+                *(uint32_t*)to = at8(0) | at8(1) << 8 | at8(2) << 16 | at8(3) << 24;
+            } else if constexpr (P::kBytes == 2) {
+                auto at16 = [&](int j) { return (uint32_t) * (const uint16_t*)(from + j * next); };
+                *(u32x2*)to = u32x2{at16(0) | at16(1) << 16, at16(2) | at16(3) << 16};
+            } else {
+                auto at32 = [&](int j) { return *(const uint32_t*)(from + j * next); };
+                *(u32x4*)to = u32x4{at32(0), at32(1), at32(2), at32(3)};
+            }
         } else {
-            const auto at32 = [&](int j) { return *(const uint32_t*)(from + j * next); };
-            if (n == 4) *(u32x4*)dst = u32x4{at32(0), at32(1), at32(2), at32(3)};
-            else *(uint32_t*)dst = *(const uint32_t*)from;
+            for (int j = max(0, -first); j < 4 && first + j < kTok; ++j) {
+                if (place[first + j] < 0) continue;
+                char* to = dst(place[first + j]);
+                if constexpr (P::kBytes == 1) *to = from[j * next];
+                else if constexpr (P::kBytes == 2) *(uint16_t*)to = *(const uint16_t*)(from + j * next);
+                else *(uint32_t*)to = *(const uint32_t*)(from + j * next);
+            }
         }
     }
 }
@@ -316,55 +319,137 @@ int launch_cache_append(const mmoe_cache_shape& s, const mmoe_cache_rows& rows, 
     return launch_status();
 }
 
-// A thread reads 16 elements of a row's keys or values back: adjacent threads have adjacent rows, whose pieces are neighbours.
-template <int FORMAT, bool F32>
+// A wavefront reads the keys or the values of one head and of 64 of the listed places back.  The first of them is chosen so that, where
+// the list starts with a run of places, a wavefront has one page's.
+template <int FORMAT, bool F32, int DG>
 __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, const char* __restrict__ v, const float* __restrict__ ks,
                                                    const float* __restrict__ vs, const int32_t* __restrict__ places,
-                                                   char* __restrict__ K, char* __restrict__ V, int R, int heads, int D, int64_t n_places)
+                                                   char* __restrict__ K, char* __restrict__ V, int R, int heads, int D, int64_t n_places,
+                                                   bool aligned)
 {
     using P = Kept<FORMAT, F32>;
-    constexpr int kEsz = F32 ? 4 : 2;
-    const int U = D / 16, h = blockIdx.y, which = blockIdx.z;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = id / (16 * U) * 16 + id % 16;  // 16 rows, unit by unit
-    const int u = (int)(id / 16 % U);
-    if (r >= R) return;
-    const int p = places[r];
-    float x[16];
-    if (p < 0 || p >= n_places) {
+    constexpr int kEsz = F32 ? 4 : 2, E = P::E;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int which = (int)(item & 1), h = (int)((item >> 1) % heads);
+    const int64_t tile = (item >> 1) / heads;
+    const int64_t r0 = tile * 64 - (aligned ? places[0] & (kPage - 1) : 0);  // first row of the list; rows before 0 and from R on are not there
+    if (r0 >= R) return;  // uniform
+    const int64_t mine = r0 + lane;
+    const bool listed = mine >= 0 && mine < R;
+    int p = listed ? places[mine] : -1;
+    if (p >= n_places || p < 0) p = -1;
+    const uint64_t all = __ballot(listed);
+    // values as fp32 from a piece
+    auto value = [&](const u32x4& x, int i) {
+        if constexpr (P::kPlain && F32) return __uint_as_float(x[i]);
+        else if constexpr (P::kPlain) return i & 1 ? bf16_hi(x[i / 2]) : bf16_lo(x[i / 2]);
+        else return value_of<FORMAT>((x[i / 4] >> (i % 4 * 8)) & 0xFF);
+    };
+    if (which == 0) {
+        // 16 rows by 4 units of 16 elements at a time: pieces of adjacent rows are neighbours
+        const int U = D / 16;
+        for (int part = 0; part < 4; ++part) {
+            if (!(all >> (part * 16) & 0xFFFF)) continue;  // uniform
+            const int row = part * 16 + (lane & 15);
+            const int64_t r = r0 + row;
+            const int q = __shfl(p, row);
+            const bool there = r >= 0 && r < R;
+            const int64_t ph = (int64_t)(max(q, 0) / kPage) * heads + h;
+            const char* base = k + ph * kPage * D * P::kBytes;
+            float scale = 1.0f;
+            if constexpr (!P::kPlain) scale = q >= 0 ? ks[ph * kPage + q % kPage] : 0.0f;
+            for (int u = lane >> 4; u < U; u += 4) {
+                float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-    } else {
-        const int64_t ph = (int64_t)(p / kPage) * heads + h;
-        const char* base = (which ? v : k) + ph * kPage * D * P::kBytes;
-        float scale = 1.0f;
-        if constexpr (!P::kPlain) scale = (which ? vs : ks)[ph * kPage + p % kPage];
+                for (int i = 0; i < 16 / E; ++i) {
+                    const u32x4 piece = *(const u32x4*)(base + (int64_t)P::k_at(max(q, 0) % kPage, 16 * u + i * E, D) * P::kBytes);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const char* at = base + (int64_t)(which ? P::v_at(p % kPage, 16 * u + i) : P::k_at(p % kPage, 16 * u + i, D)) * P::kBytes;
-            if constexpr (P::kPlain && F32) x[i] = *(const float*)at;
-            else if constexpr (P::kPlain) x[i] = bf16_bits_to_f32(*(const uint16_t*)at);
-            else x[i] = value_of<FORMAT>(*(const uint8_t*)at) * scale;
+                    for (int j = 0; j < E; ++j) x[i * E + j] = q >= 0 ? value(piece, j) * scale : 0.0f;
+                }
+                if (there) {
+                    char* out = K + ((r * heads + h) * D + 16 * u) * kEsz;
+                    store8<F32>(out, x);
+                    store8<F32>(out + 8 * kEsz, x + 8);
+                }
+            }
+        }
+        return;
+    }
+    // Values: runs of places on one page, each read as whole pieces.  Lane (g, c) has the rows 16 q + 4 g + e of the page and D/16
+    // elements.
+    const int before = __shfl_up(p, 1);
+    uint64_t starts = __ballot(listed && (lane == 0 || p < 0 || p != before + 1 || (p & (kPage - 1)) == 0 || mine == 0));
+    const int g = lane & 3, c = lane >> 2, n = D / 16;
+    while (starts) {
+        const int first = __ffsll((unsigned long long)starts) - 1;
+        starts &= starts - 1;
+        const int next = starts ? __ffsll((unsigned long long)starts) - 1 : 64 - __clzll((long long)all);
+        const int place = __shfl(p, first);                    // uniform
+        const int begin = place & (kPage - 1), count = next - first;  // rows begin .. of the page are rows first .. of the tile
+        const int64_t ph = (int64_t)(max(place, 0) / kPage) * heads + h;
+        const char* base = v + ph * kPage * D * P::kBytes;
+        char* out = V + ((r0 + first - begin) * heads + h) * D * kEsz;  // of the page's row 0
+        if (place < 0) {
+            for (int i = lane; i < count * D; i += 64) {
+                char* to = V + (((r0 + first + i / D) * heads + h) * D + i % D) * kEsz;
+                if (F32) *(float*)to = 0.0f;
+                else *(uint16_t*)to = 0;
+            }
+            continue;
+        }
+        f32x4 scale[4];
+        if constexpr (!P::kPlain)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) scale[q] = *(const f32x4*)(vs + ph * kPage + q * 16 + g * 4);
+        for (int d0 = c * n; d0 < (c + 1) * n; d0 += DG) {  // DG elements of 16 rows
+            u32x4 piece[DG][16 / E];
+#pragma unroll
+            for (int i = 0; i < DG; ++i)
+#pragma unroll
+                for (int j = 0; j < 16 / E; ++j)
+                    piece[i][j] = *(const u32x4*)(base + ((((int64_t)(d0 + i) >> 4) * (16 / E) + j) * 64 + g * 16 + ((d0 + i) & 15)) * 16);
+            each<16>([&](auto atc) {
+                constexpr int at = decltype(atc)::value, q = at / 4, e = at % 4;
+                const int row = q * 16 + g * 4 + e;
+                if (row < begin || row >= begin + count) return;
+                float x[DG];
+                each<DG>([&](auto i) {
+                    x[decltype(i)::value] = value(piece[decltype(i)::value][at / E], at % E);
+                    if constexpr (!P::kPlain) x[decltype(i)::value] *= scale[q][e];
+                });
+                char* to = out + ((int64_t)row * heads * D + d0) * kEsz;
+                if constexpr (DG == 8) store8<F32>(to, x);
+                else if constexpr (F32) *(f32x4*)to = f32x4{x[0], x[1], x[2], x[3]};
+                else *(u32x2*)to = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+            });
         }
     }
-    char* out = (which ? V : K) + ((r * heads + h) * D + 16 * u) * kEsz;
-    store8<F32>(out, x);
-    store8<F32>(out + 8 * kEsz, x + 8);
+}
+
+template <int FORMAT, bool F32>
+static void read_back(const mmoe_cache_shape& s, const mmoe_cache& c, int R, const int32_t* places, void* K, void* V, hipStream_t st)
+{
+    // A list of more than a few pages is taken from the page of its first place on; in a short one that look costs a microsecond.
+    const bool aligned = R > 4 * kPage;
+    const int64_t items = ((int64_t)(R + kPage - 1) / 64 + (aligned ? 1 : 0)) * s.kv_heads * 2;
+    const dim3 grid((unsigned)((items + 3) / 4)), block(256);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, st, (const char*)c.k, (const char*)c.v, c.k_scale, c.v_scale, places, (char*)K, (char*)V,
+                           R, s.kv_heads, s.head_dim, (int64_t)s.n_pages * kPage, aligned);
+    };
+    if (s.head_dim == 64 || F32) go(read_kernel<FORMAT, F32, 4>);
+    else go(read_kernel<FORMAT, F32, F32 ? 4 : 8>);
 }
 
 int launch_cache_read(const mmoe_cache_shape& s, const mmoe_cache& c, int R, const int32_t* places, void* K, void* V, hipStream_t st)
 {
-    const int U = s.head_dim / 16;
-    const dim3 grid((unsigned)(((int64_t)(R + 15) / 16 * 16 * U + 255) / 256), s.kv_heads, 2), block(256);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, block, 0, st, (const char*)c.k, (const char*)c.v, c.k_scale, c.v_scale, places, (char*)K, (char*)V,
-                           R, s.kv_heads, s.head_dim, (int64_t)s.n_pages * kPage);
-    };
     const bool f32 = s.dtype == MMOE_F32;
+    auto go = [&](auto read) { read(s, c, R, places, K, V, st); };
     switch (s.format) {
-        case MMOE_CACHE_PLAIN: f32 ? go(read_kernel<MMOE_CACHE_PLAIN, true>) : go(read_kernel<MMOE_CACHE_PLAIN, false>); break;
-        case MMOE_CACHE_INT8: f32 ? go(read_kernel<MMOE_CACHE_INT8, true>) : go(read_kernel<MMOE_CACHE_INT8, false>); break;
-        default: f32 ? go(read_kernel<MMOE_CACHE_FP8, true>) : go(read_kernel<MMOE_CACHE_FP8, false>); break;
+        case MMOE_CACHE_PLAIN: f32 ? go(read_back<MMOE_CACHE_PLAIN, true>) : go(read_back<MMOE_CACHE_PLAIN, false>); break;
+        case MMOE_CACHE_INT8: f32 ? go(read_back<MMOE_CACHE_INT8, true>) : go(read_back<MMOE_CACHE_INT8, false>); break;
+        default: f32 ? go(read_back<MMOE_CACHE_FP8, true>) : go(read_back<MMOE_CACHE_FP8, false>); break;
     }
     return launch_status();
 }
