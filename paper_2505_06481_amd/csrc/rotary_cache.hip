@@ -163,7 +163,7 @@ struct AppendArgs {
     char *k, *v;
     float *k_scale, *v_scale;
     int64_t kt, kh, vt, vh;  // strides
-    int T, heads, D, rot;
+    int T, heads, rot;
     int64_t n_places;
     float m, sign;
 };
@@ -171,15 +171,15 @@ struct AppendArgs {
 // A workgroup appends 16 tokens of one head: thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8
 // each in one piece; values, whose pieces hold several tokens, through LDS, where four tokens in consecutive places become one store.
 // ROTATE: 0 no, 1 halves, 2 neighbours.
-template <int FORMAT, bool F32, int ROTATE>
-__global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
+template <int FORMAT, bool F32, int ROTATE, int D>
+__global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs g)
 {
     using P = Kept<FORMAT, F32>;
     constexpr int kEsz = F32 ? 4 : 2, kTok = 16;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int U = g.D / 16, nthreads = 2 * kTok * U, tid = threadIdx.x;
-    char* codes = lds;                                      // [kTok][D] of V
-    float* amax = (float*)(lds + kTok * g.D * P::kBytes);   // [2][kTok][U]
+    constexpr int U = D / 16, kThreads = 2 * kTok * U;
+    const int tid = threadIdx.x;
+    __shared__ __attribute__((aligned(16))) char codes[kTok * D * P::kBytes];  // [kTok][D] of V
+    __shared__ float amax[P::kPlain ? 1 : 2 * kTok * U];                        // [2][kTok][U]
     __shared__ int place[kTok];
     const int t0 = blockIdx.x * kTok, h = blockIdx.y;
     const int which = tid / (kTok * U), tok = tid / U % kTok, u = tid % U;  // which: 0 keys, 1 values
@@ -222,18 +222,24 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
         for (int i = 0; i < 16; ++i) code[i] = code_of<FORMAT>(fine ? x[i] * inv : 0.0f);
         if (u == 0 && p >= 0) (which ? g.v_scale : g.k_scale)[((int64_t)(p / kPage) * g.heads + h) * kPage + p % kPage] = scale;
     }
-    const int64_t block = (int64_t)kPage * g.D;
+    const int64_t block = (int64_t)kPage * D;
     if (which == 0) {
         if (p >= 0) {
             char* k = g.k + ((int64_t)(p / kPage) * g.heads + h) * block * P::kBytes;
+            if constexpr (!P::kPlain && ROTATE != 1) {  // 16 codes in a row are a piece
+                u32x4 piece;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) piece[i] = code[4 * i] | code[4 * i + 1] << 8 | code[4 * i + 2] << 16 | code[4 * i + 3] << 24;
+                *(u32x4*)(k + (int64_t)P::k_at(p % kPage, 16 * u, D)) = piece;
+            } else
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int d = half ? at.b : at.a;
-                char* dst = k + (int64_t)P::k_at(p % kPage, d, g.D) * P::kBytes;
+                char* dst = k + (int64_t)P::k_at(p % kPage, d, D) * P::kBytes;
                 const float* v = x + 8 * half;
                 if constexpr (P::kPlain && F32) {
                     *(f32x4*)dst = f32x4{v[0], v[1], v[2], v[3]};
-                    *(f32x4*)(k + (int64_t)P::k_at(p % kPage, d + 4, g.D) * 4) = f32x4{v[4], v[5], v[6], v[7]};
+                    *(f32x4*)(k + (int64_t)P::k_at(p % kPage, d + 4, D) * 4) = f32x4{v[4], v[5], v[6], v[7]};
                 } else if constexpr (P::kPlain) {
                     store8<false>(dst, v);
                 } else {
@@ -243,7 +249,7 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
             }
         }
     } else {
-        char* row = codes + (tok * g.D + 16 * u) * P::kBytes;
+        char* row = codes + (tok * D + 16 * u) * P::kBytes;
         if constexpr (P::kPlain) {
             store8<F32>(row, x);
             store8<F32>(row + 8 * kEsz, x + 8);
@@ -257,10 +263,10 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
     // Four tokens that stand in consecutive places, the first in a multiple of four, are one store for each element; they start at the
     // first token's distance from such a place.
     const int shift = -place[0] & 3;
-    for (int i = tid; i < (kTok / 4 + 1) * g.D; i += nthreads) {
-        const int d = i % g.D, first = (i / g.D - 1) * 4 + shift;  // token of the group's first place; the group may begin before the tile
-        const int next = g.D * P::kBytes;
-        const char* from = codes + (first * g.D + d) * P::kBytes;
+    for (int i = tid; i < (kTok / 4 + 1) * D; i += kThreads) {
+        const int d = i % D, first = (i / D - 1) * 4 + shift;  // token of the group's first place; the group may begin before the tile
+        const int next = D * P::kBytes;
+        const char* from = codes + (first * D + d) * P::kBytes;
         auto dst = [&](int q) { return g.v + (((int64_t)(q / kPage) * g.heads + h) * block + P::v_at(q % kPage, d)) * P::kBytes; };
         bool whole = first >= 0 && first + 3 < kTok && place[first] >= 0 && (place[first] & 3) == 0;
         if (whole)
@@ -290,15 +296,21 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs g)
     }
 }
 
-template <int FORMAT, bool F32>
-static void append(const mmoe_rotary_shape* rotary, const AppendArgs& g, hipStream_t st)
+template <int FORMAT, bool F32, int D>
+static void append_wide(const mmoe_rotary_shape* rotary, const AppendArgs& g, hipStream_t st)
 {
-    const int U = g.D / 16, kept = Kept<FORMAT, F32>::kBytes;
-    const dim3 grid((g.T + 15) / 16, g.heads), block(2 * 16 * U);
-    const size_t lds = (size_t)16 * g.D * kept + 2 * 16 * U * sizeof(float);
-    if (!rotary) hipLaunchKernelGGL((append_kernel<FORMAT, F32, 0>), grid, block, lds, st, g);
-    else if (rotary->layout == MMOE_ROTARY_HALVES) hipLaunchKernelGGL((append_kernel<FORMAT, F32, 1>), grid, block, lds, st, g);
-    else hipLaunchKernelGGL((append_kernel<FORMAT, F32, 2>), grid, block, lds, st, g);
+    const dim3 grid((g.T + 15) / 16, g.heads), block(2 * D);
+    if (!rotary) hipLaunchKernelGGL((append_kernel<FORMAT, F32, 0, D>), grid, block, 0, st, g);
+    else if (rotary->layout == MMOE_ROTARY_HALVES) hipLaunchKernelGGL((append_kernel<FORMAT, F32, 1, D>), grid, block, 0, st, g);
+    else hipLaunchKernelGGL((append_kernel<FORMAT, F32, 2, D>), grid, block, 0, st, g);
+}
+
+template <int FORMAT, bool F32>
+static void append(int D, const mmoe_rotary_shape* rotary, const AppendArgs& g, hipStream_t st)
+{
+    if (D == 64) append_wide<FORMAT, F32, 64>(rotary, g, st);
+    else if (D == 128) append_wide<FORMAT, F32, 128>(rotary, g, st);
+    else append_wide<FORMAT, F32, 256>(rotary, g, st);
 }
 
 int launch_cache_append(const mmoe_cache_shape& s, const mmoe_cache_rows& rows, const void* K, const void* V, const int32_t* places,
@@ -308,27 +320,28 @@ int launch_cache_append(const mmoe_cache_shape& s, const mmoe_cache_rows& rows, 
     const int64_t hd = s.head_dim, td = (int64_t)s.kv_heads * s.head_dim;
     AppendArgs g = {(const char*)K, (const char*)V, places, pos, steps, (char*)cache.k, (char*)cache.v, cache.k_scale, cache.v_scale,
                     rows.k_token ? rows.k_token : td, rows.k_head ? rows.k_head : hd, rows.v_token ? rows.v_token : td,
-                    rows.v_head ? rows.v_head : hd, rows.T, s.kv_heads, s.head_dim, rotary ? rotary->rot : 0,
+                    rows.v_head ? rows.v_head : hd, rows.T, s.kv_heads, rotary ? rotary->rot : 0,
                     (int64_t)s.n_pages * kPage, rotary ? rotary->magnitude : 1.0f, rotary && rotary->transpose ? -1.0f : 1.0f};
     const bool f32 = s.dtype == MMOE_F32;
     switch (s.format) {
-        case MMOE_CACHE_PLAIN: f32 ? append<MMOE_CACHE_PLAIN, true>(rotary, g, st) : append<MMOE_CACHE_PLAIN, false>(rotary, g, st); break;
-        case MMOE_CACHE_INT8: f32 ? append<MMOE_CACHE_INT8, true>(rotary, g, st) : append<MMOE_CACHE_INT8, false>(rotary, g, st); break;
-        default: f32 ? append<MMOE_CACHE_FP8, true>(rotary, g, st) : append<MMOE_CACHE_FP8, false>(rotary, g, st); break;
+        case MMOE_CACHE_PLAIN: f32 ? append<MMOE_CACHE_PLAIN, true>(s.head_dim, rotary, g, st) : append<MMOE_CACHE_PLAIN, false>(s.head_dim, rotary, g, st); break;
+        case MMOE_CACHE_INT8: f32 ? append<MMOE_CACHE_INT8, true>(s.head_dim, rotary, g, st) : append<MMOE_CACHE_INT8, false>(s.head_dim, rotary, g, st); break;
+        default: f32 ? append<MMOE_CACHE_FP8, true>(s.head_dim, rotary, g, st) : append<MMOE_CACHE_FP8, false>(s.head_dim, rotary, g, st); break;
     }
     return launch_status();
 }
 
 // A wavefront reads the keys or the values of one head and of 64 of the listed places back.  The first of them is chosen so that, where
 // the list starts with a run of places, a wavefront has one page's.
-template <int FORMAT, bool F32, int DG>
+template <int FORMAT, bool F32, int D>
 __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, const char* __restrict__ v, const float* __restrict__ ks,
                                                    const float* __restrict__ vs, const int32_t* __restrict__ places,
-                                                   char* __restrict__ K, char* __restrict__ V, int R, int heads, int D, int64_t n_places,
+                                                   char* __restrict__ K, char* __restrict__ V, int R, int heads, int64_t n_places,
                                                    bool aligned)
 {
     using P = Kept<FORMAT, F32>;
     constexpr int kEsz = F32 ? 4 : 2, E = P::E;
+    constexpr int DG = D == 64 || F32 ? 4 : 8;  // elements of a row that a lane stores at once: 16 bytes (8 for heads of 64)
     const int lane = threadIdx.x & 63;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int which = (int)(item & 1), h = (int)((item >> 1) % heads);
@@ -348,7 +361,7 @@ __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, c
     };
     if (which == 0) {
         // 16 rows by 4 units of 16 elements at a time: pieces of adjacent rows are neighbours
-        const int U = D / 16;
+        constexpr int U = D / 16;
         for (int part = 0; part < 4; ++part) {
             if (!(all >> (part * 16) & 0xFFFF)) continue;  // uniform
             const int row = part * 16 + (lane & 15);
@@ -380,7 +393,8 @@ __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, c
     // elements.
     const int before = __shfl_up(p, 1);
     uint64_t starts = __ballot(listed && (lane == 0 || p < 0 || p != before + 1 || (p & (kPage - 1)) == 0 || mine == 0));
-    const int g = lane & 3, c = lane >> 2, n = D / 16;
+    const int g = lane & 3, c = lane >> 2;
+    constexpr int n = D / 16;
     while (starts) {
         const int first = __ffsll((unsigned long long)starts) - 1;
         starts &= starts - 1;
@@ -436,10 +450,11 @@ static void read_back(const mmoe_cache_shape& s, const mmoe_cache& c, int R, con
     const dim3 grid((unsigned)((items + 3) / 4)), block(256);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, block, 0, st, (const char*)c.k, (const char*)c.v, c.k_scale, c.v_scale, places, (char*)K, (char*)V,
-                           R, s.kv_heads, s.head_dim, (int64_t)s.n_pages * kPage, aligned);
+                           R, s.kv_heads, (int64_t)s.n_pages * kPage, aligned);
     };
-    if (s.head_dim == 64 || F32) go(read_kernel<FORMAT, F32, 4>);
-    else go(read_kernel<FORMAT, F32, F32 ? 4 : 8>);
+    if (s.head_dim == 64) go(read_kernel<FORMAT, F32, 64>);
+    else if (s.head_dim == 128) go(read_kernel<FORMAT, F32, 128>);
+    else go(read_kernel<FORMAT, F32, 256>);
 }
 
 int launch_cache_read(const mmoe_cache_shape& s, const mmoe_cache& c, int R, const int32_t* places, void* K, void* V, hipStream_t st)
