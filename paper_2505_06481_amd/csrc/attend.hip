@@ -4,18 +4,22 @@
 
 namespace mmoe {
 
-constexpr int kLeastPages = 16;   // of a share
 constexpr int kMaxShares = 4096;
+constexpr int kManyParts = 8;  // of a request on average: four wavefronts join them
 
-// Joins the parts of a request that several shares have: a wavefront takes a (token, head).
-template <int D, bool F32>
+// Joins the parts of a request that several shares have: WPR wavefronts take a (token, head), each every WPR-th part.
+template <int D, bool F32, int WPR>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 {
-    __shared__ int sums[256][2];
-    const int tid = threadIdx.x, per = (min(g.max_drafts, g.T) * g.heads + 3) / 4, b = blockIdx.x / per;
+    __shared__ int sums[4][2];
+    __shared__ float parts[WPR == 1 ? 1 : 4][D + 1];
+    constexpr int kRows = 4 / WPR;  // of a workgroup
+    const int tid = threadIdx.x, per = (min(g.max_drafts, g.T) * g.heads + kRows - 1) / kRows, b = blockIdx.x / per;
+    const int lane = tid & 63, wave = tid >> 6, mine = wave % WPR;
     const Request r = request_of(g, b);
-    const int row = blockIdx.x % per * 4 + (tid >> 6), lane = tid & 63;  // token of the request, head
-    if (blockIdx.x % per * 4 >= r.n * g.heads) return;  // uniform
+    const int rows = r.n * g.heads, row0 = blockIdx.x % per * kRows;
+    if (row0 >= rows || !r.pages) return;              // uniform
+    const int row = min(row0 + wave / WPR, rows - 1);  // token of the request, head; the last one again where there are no more
     int before = 0, all = 0;
     for (int i = tid; i < g.B; i += 256) {
         const int pages = request_of(g, i).pages;
@@ -25,23 +29,19 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 #define MMOE_JOIN(OFF) all += lane_xor<OFF>(all), before += lane_xor<OFF>(before)
     MMOE_JOIN(1); MMOE_JOIN(2); MMOE_JOIN(4); MMOE_JOIN(8); MMOE_JOIN(16); MMOE_JOIN(32);
 #undef MMOE_JOIN
-    if (lane == 0) sums[tid >> 6][0] = all, sums[tid >> 6][1] = before;
+    if (lane == 0) sums[wave][0] = all, sums[wave][1] = before;
     __syncthreads();
     const int P = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], p0 = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
-    if (row >= r.n * g.heads || !r.pages) return;
     // shares of the request's first and last page
     const Cut cut(P, g.shares);
     const int w0 = cut.of(p0), w1 = cut.of(p0 + r.pages - 1);
     if (w0 == w1) return;  // written by the share that has it all
     const int64_t t = r.start + row / g.heads;
     const int head = row % g.heads, h = head / g.G, c = row / g.heads * g.G + head % g.G;
-    auto part = [&](int w) {
-        const int slot = w == w0 && cut.start(w) < p0 ? 1 : 0;
-        return (((int64_t)w * 2 + slot) * g.kv_heads + h) * g.columns + c;
-    };
+    const int slot0 = cut.start(w0) < p0 ? 1 : 0;
+    auto part = [&](int w) { return (((int64_t)w * 2 + (w == w0 ? slot0 : 0)) * g.kv_heads + h) * g.columns + c; };
     float top = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 64)
-        top = fmaxf(top, g.part_ml[part(w) * 2]);
+    for (int w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, g.part_ml[part(w) * 2]);
 #define MMOE_JOIN(OFF) top = fmaxf(top, lane_xor<OFF>(top))
     MMOE_JOIN(1); MMOE_JOIN(2); MMOE_JOIN(4); MMOE_JOIN(8); MMOE_JOIN(16); MMOE_JOIN(32);
 #undef MMOE_JOIN
@@ -51,12 +51,25 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
 #pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
+    for (int w = w0 + mine; w <= w1; w += WPR) {
         const int64_t at = part(w);
         const float f = pow2(g.part_ml[at * 2] - base);
         l += f * g.part_ml[at * 2 + 1];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) x[i] += f * g.part_o[at * D + i * 64 + lane];
+    }
+    if constexpr (WPR > 1) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) parts[wave][i * 64 + lane] = x[i];
+        if (lane == 0) parts[wave][D] = l;
+        __syncthreads();
+        if (mine) return;
+#pragma unroll
+        for (int v = 1; v < WPR; ++v) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] += parts[wave + v][i * 64 + lane];
+            l += parts[wave + v][D];
+        }
     }
     const float inv = l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
@@ -75,23 +88,35 @@ static Shares shares_of(const mmoe_attend_shape& s)
     const int64_t C = (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * G;
     r.cols = C > 16 * most;
     const int64_t per = r.cols ? (C + 3) / 4 : C;
-    r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : !r.cols && per <= 48 ? 3 : 4;
+    r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : per <= 48 ? 3 : 4;
     const int wide = 16 * r.nc * (r.cols ? 4 : 1);
     r.groups = (int)((C + wide - 1) / wide);
     const int64_t cap = (int64_t)s.max_pages * kPage;
     const int64_t longest = s.max_keys && s.max_keys < cap ? s.max_keys : cap;
     const int64_t sum = s.sum_keys ? s.sum_keys : (int64_t)s.n_requests * longest;
     const int64_t pages = sum / kPage + s.n_requests, most_pages = (longest + kPage - 1) / kPage;
-    // workgroups that are resident at once, for each key head and column group
+    // Estimated cycles: a page to a wavefront (its memory share and NC times the work on 16 columns), a request that a workgroup
+    // takes up, and the join (more where a request has many parts).  Wavefronts with different keys take four pages at once.
+    const double wide_heads = s.cache.head_dim / 128.0;
+    const double page = s.cache.format != MMOE_CACHE_PLAIN ? 2000.0 + 1500.0 * r.nc * wide_heads
+                        : s.cache.dtype == MMOE_BF16       ? 2500.0 + 1400.0 * r.nc * wide_heads
+                                                           : 3000.0 + 8500.0 * r.nc * wide_heads;
+    constexpr double kRequest = 12000.0, kJoin = 14000.0;
     const int64_t room = 256 * (r.nc == 1 && s.cache.head_dim <= 128 ? 2 : 1), heads = (int64_t)s.cache.kv_heads * r.groups;
-    int64_t w = room / heads;
-    if (w < s.n_requests) w = s.n_requests;
-    if (w > pages / kLeastPages) w = pages / kLeastPages;
-    if (w > kMaxShares) w = kMaxShares;
-    // One workgroup to a request where the longest request is not what the call would wait for.
-    const int64_t rounds = (s.n_requests * heads + room - 1) / room;
-    const bool even = most_pages <= kLeastPages || most_pages * room <= pages * heads + (rounds > 1 ? pages * heads / 4 : 0);
-    r.shares = even || s.n_requests > kMaxShared || w <= 1 || s.n_requests * (int64_t)s.max_pages >= (int64_t)1 << 30 ? 0 : (int)w;
+    auto work = [&](double n) { return r.cols ? n * page : ceil(n / 4.0) * page; };  // n pages
+    const double even = work((double)pages * heads / room);                         // all of it, spread evenly
+    double least = kRequest * ((s.n_requests * heads + room - 1) / room) + (work((double)most_pages) > even ? work((double)most_pages) : even);
+    r.shares = 0;
+    if (s.n_requests <= kMaxShared && s.n_requests * (int64_t)s.max_pages < (int64_t)1 << 30) {
+        // rounds of resident workgroups, or shares of a few pages
+        const int64_t tries[] = {room / heads, 2 * room / heads, 3 * room / heads, 4 * room / heads, pages / 4, pages / 8, pages / 16, pages / 32};
+        for (int64_t w : tries) {
+            if (w < 2 || w > kMaxShares || w > pages) continue;
+            const double each = (double)pages / w, taken = 1.0 + (double)s.n_requests / w;  // pages, requests of a share
+            const double time = (double)((w * heads + room - 1) / room) * (taken * (work(each / taken) + kRequest)) + kJoin + 200.0 * w / s.n_requests;
+            if (time < least) least = time, r.shares = (int)w;
+        }
+    }
     return r;
 }
 
@@ -100,7 +125,7 @@ bool attend_fits(const mmoe_attend_shape& s)
 {
     const Shares r = shares_of(s);
     const int64_t drafts = s.max_drafts < s.T ? s.max_drafts : s.T, most = ((int64_t)1 << 31) - 1;
-    return drafts * s.heads < most && (drafts * s.heads + 3) / 4 * s.n_requests <= most &&
+    return drafts * s.heads < most && drafts * s.heads * s.n_requests <= most &&
            ((int64_t)s.cache.kv_heads * (r.shares ? r.shares : s.n_requests) + 8) * r.groups <= most;
 }
 
@@ -128,11 +153,19 @@ int launch_attend(const mmoe_attend_shape& s, const void* Q, const int32_t* star
     (s.cache.format == MMOE_CACHE_INT8 ? attend_int8 : s.cache.format == MMOE_CACHE_FP8 ? attend_fp8 : f32 ? attend_f32 : attend_bf16)((int)D, r, g, st);
     if (r.shares) {
         const int64_t drafts = s.max_drafts < s.T ? s.max_drafts : s.T;
-        const dim3 grid((unsigned)((drafts * s.heads + 3) / 4 * s.n_requests)), block(256);
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
-        if (D == 64) f32 ? go(attend_join_kernel<64, true>) : go(attend_join_kernel<64, false>);
-        else if (D == 128) f32 ? go(attend_join_kernel<128, true>) : go(attend_join_kernel<128, false>);
-        else f32 ? go(attend_join_kernel<256, true>) : go(attend_join_kernel<256, false>);
+        auto go = [&](auto kernel, int rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((drafts * s.heads + rows - 1) / rows * s.n_requests)), dim3(256), 0, st, g);
+        };
+        auto wide = [&](auto d, auto f) {
+            constexpr int kD = decltype(d)::value;
+            constexpr bool kF = decltype(f)::value;
+            if (r.shares >= kManyParts * (int64_t)s.n_requests) go(attend_join_kernel<kD, kF, 4>, 1);
+            else go(attend_join_kernel<kD, kF, 1>, 4);
+        };
+        auto typed = [&](auto d) { f32 ? wide(d, std::true_type{}) : wide(d, std::false_type{}); };
+        if (D == 64) typed(std::integral_constant<int, 64>{});
+        else if (D == 128) typed(std::integral_constant<int, 128>{});
+        else typed(std::integral_constant<int, 256>{});
     }
     return launch_status();
 }

@@ -147,7 +147,12 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     constexpr int NP = KT * 4 / (KIND == kF32 ? 4 : 8);  // operand pieces of the probabilities
     constexpr bool kCodes = L::kCodes;
     constexpr int kEsz = KIND == kF32 ? 4 : 2;  // of Q and out
-    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    // What follows from the lane is worked out where it is used: hoisted out of the loops, it would push operands out of registers.
+    auto fresh = [](int x) {
+        asm volatile("" : "+v"(x));
+        return x;
+    };
+    int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     // column groups of the same keys on one XCD (workgroup id mod 8)
@@ -209,6 +214,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     }
     const int share_at = at;
   for (; at < until; ++b) {  // requests of the share
+    tid = fresh(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const Request r = request_of(g, b);
     const int start = r.start, n = r.n, ctx = r.ctx, total = r.total, C = n * g.G;
     constexpr int kWide = COLS ? 64 * NC : 16 * NC;
@@ -536,10 +542,13 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
                                 });
                                 count = mma_kind<KIND>(mark, seen, count);
                             });
+                            f32x4 add;
                             each<4>([&](auto e) {
-                                if (count[decltype(e)::value] > 0.0f)
-                                    o[ct][dt][decltype(e)::value] += kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                                const float special = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                                add[decltype(e)::value] = count[decltype(e)::value] > 0.0f ? special : 0.0f;
                             });
+                            o[ct][dt] += add;
+                            if constexpr (attend_waves<D, KIND, NC>() == 1) in_agprs(o[ct][dt]);
                             __builtin_amdgcn_sched_barrier(0);
                         });
                     }
@@ -581,6 +590,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     }
 
     // ---- results ----
+    tid = fresh(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     if constexpr (kCodes) {
         const float down = ldexpf(1.0f, max(lift - kLiftBits, -140));
 #pragma unroll
@@ -682,7 +692,7 @@ static void attend_wide(const Shares& r, const AttendArgs& g, hipStream_t st)
     const dim3 grid((unsigned)(sets * r.groups)), block(256);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
     if (r.cols) {
-        if constexpr (D <= 128) r.nc == 2 ? go(attend_kernel<D, KIND, 2, true>) : go(attend_kernel<D, KIND, 4, true>);
+        if constexpr (D <= 128) r.nc == 2 ? go(attend_kernel<D, KIND, 2, true>) : r.nc == 3 ? go(attend_kernel<D, KIND, 3, true>) : go(attend_kernel<D, KIND, 4, true>);
         else go(attend_kernel<D, KIND, 2, true>);
     } else {
         if (r.nc == 1) go(attend_kernel<D, KIND, 1, false>);

@@ -55,6 +55,7 @@ struct ShrinkArgs {
     int64_t ldx;
     int T, K, R, Rp, n;
     int chunk;        // tokens
+    int groups;       // of a chunk
     bool by_token;    // groups are tokens (chunks of up to kScan)
 };
 constexpr int kScan = 512;  // tokens looked through at once
@@ -428,23 +429,24 @@ __global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_
         ShrinkLds shrink;
     } lds;
     if ((int)blockIdx.x < tiles) tile_body<F32, WM, WN>(g, lds.tile, blockIdx.x, tiles);
-    else shrink_body<F32>(u, lds.shrink, blockIdx.x - tiles, 0);
+    else shrink_body<F32>(u, lds.shrink, (blockIdx.x - tiles) % u.groups, (blockIdx.x - tiles) / u.groups);
 }
 
-// Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes tokens of one adapter (or of none), 16 of every
-// gridDim.z times 16, and 256 features, 64 to a wavefront.
+// Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes tokens of one adapter (or of none) among kScan, 16 of
+// every `sixteens` times 16, and 256 features, 64 to a wavefront.
 template <bool F32>
-__global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool by_token)
+__global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool by_token, int sixteens)
 {
     constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
     __shared__ int list[kScan], shared_count;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
-    const int a = adapter_of(g.aid, 0, g.T, blockIdx.y, by_token, g.n);
+    const int t0 = blockIdx.z / sixteens * kScan, some = min(kScan, g.T - t0);
+    const int a = adapter_of(g.aid, t0, some, blockIdx.y, by_token, g.n);
     if (a < 0) return;  // uniform
-    const int count = tokens_of(g.aid, 0, g.T, a, g.n, list, &shared_count);
+    const int count = tokens_of(g.aid, t0, some, a, g.n, list, &shared_count);
     const int nb = (blockIdx.x * 4 + wave) * 4, rs = a < g.n ? g.Rp * kEsz / 64 : 0;
     const char* b = g.Bp + ((int64_t)a * (g.N / 16) + nb) * rs * 1024 + lane * 16;
-    for (int at = blockIdx.z * 16; at < count; at += gridDim.z * 16) {
+    for (int at = blockIdx.z % sixteens * 16; at < count; at += sixteens * 16) {
         const int64_t t = list[min(at + lr, count - 1)];
         const float* part = g.part + t * g.N + nb * 16 + lg * 4;
         f32x4 acc[4];
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool b
 
 // Few tokens run in two launches: parts of X W beside U, then their join with U B.  More in two as well: U, then tiles
 // that add U B themselves.
-constexpr int kFewTokens = kScan;
+constexpr int kFewTokens = 4096;
 struct ProjectPlan {
     int wm, wn, splits;
     bool few;
@@ -503,7 +505,7 @@ static ProjectPlan project_plan(const mmoe_project_shape& s)
         const double matrix = f32 ? t.wm * t.wn * 135.0 : 0.0;
         for (int splits = 0; splits <= most; ++splits) {  // 0: not in parts
             // beside the parts run the workgroups that make U
-            const int64_t wgs = splits ? n * splits + (s.n_adapters < T ? s.n_adapters : T) : n, room = t.two > 0.0 ? 512 : 256, full = wgs / room, rest = wgs % room;
+            const int64_t wgs = splits ? n * splits + (s.n_adapters < T ? s.n_adapters : T) * ((T + kScan - 1) / kScan) : n, room = t.two > 0.0 ? 512 : 256, full = wgs / room, rest = wgs % room;
             const double steps = (double)slices / (splits ? splits : 1);
             const double alone = (t.alone > matrix ? t.alone : matrix) * steps + t.ends;
             const double two = (t.two > 2.0 * matrix ? t.two : 2.0 * matrix) * steps + t.ends;
@@ -550,21 +552,24 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
     const ProjectPlan p = project_plan(s);
     ProjectArgs g = {(const char*)X, (const char*)Wp, (const char*)Bp, (const char*)ws, (char*)Y, p.few ? (float*)((char*)ws + u_bytes(s)) : nullptr, aid,
                      ldx, ldy, s.T, s.d_in, s.d_out, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
-    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, false};
+    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, n, false};
     const int tiles = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
     const dim3 block(256);
     if (p.few) {
-        const bool by_token = n + 1 > s.T;
+        const int chunk = s.T < kScan ? s.T : kScan, chunks = (s.T + kScan - 1) / kScan;
+        const bool by_token = n + 1 > chunk;
         u.by_token = by_token;
-        const dim3 grid(tiles + (n ? by_token ? s.T : n : 0));
+        u.chunk = chunk;
+        u.groups = by_token ? chunk : n;
+        const dim3 grid(tiles + (n ? u.groups * chunks : 0));
         auto parts = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g, u, tiles); };
         if (p.wm == 8) parts(project_parts_kernel<F32, 8, 8>);
         else if (p.wn == 8) parts(project_parts_kernel<F32, 4, 8>);
         else if (p.wm == 4) parts(project_parts_kernel<F32, 4, 4>);
         else parts(project_parts_kernel<F32, 2, 4>);
         // as many workgroups to an adapter as its even share of the tokens has sixteens
-        const int groups = by_token ? s.T : n + 1, share = (s.T + 16 * groups - 1) / (16 * groups);
-        hipLaunchKernelGGL(project_join_kernel<F32>, dim3(s.d_out / 256, groups, share), block, 0, st, g, by_token);
+        const int groups = by_token ? chunk : n + 1, sixteens = (chunk + 16 * groups - 1) / (16 * groups);
+        hipLaunchKernelGGL(project_join_kernel<F32>, dim3(s.d_out / 256, groups, chunks * sixteens), block, 0, st, g, by_token, sixteens);
         return;
     }
     if (n) {
