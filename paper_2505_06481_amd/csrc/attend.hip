@@ -89,6 +89,7 @@ static Shares shares_of(const mmoe_attend_shape& s)
     r.cols = C > 16 * most;
     const int64_t per = r.cols ? (C + 3) / 4 : C;
     r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : per <= 48 ? 3 : 4;
+    if (r.cols && s.cache.head_dim == 64) r.nc = 2;
     const int wide = 16 * r.nc * (r.cols ? 4 : 1);
     r.groups = (int)((C + wide - 1) / wide);
     const int64_t cap = (int64_t)s.max_pages * kPage;
@@ -102,7 +103,7 @@ static Shares shares_of(const mmoe_attend_shape& s)
                         : s.cache.dtype == MMOE_BF16       ? 2500.0 + 1400.0 * r.nc * wide_heads
                                                            : 3000.0 + 8500.0 * r.nc * wide_heads;
     constexpr double kRequest = 12000.0, kJoin = 14000.0;
-    const int64_t room = 256 * (r.nc == 1 && s.cache.head_dim <= 128 ? 2 : 1), heads = (int64_t)s.cache.kv_heads * r.groups;
+    const int64_t room = 256 * ((r.nc == 1 && s.cache.head_dim <= 128) || (r.nc == 2 && s.cache.head_dim == 64) ? 2 : 1), heads = (int64_t)s.cache.kv_heads * r.groups;
     auto work = [&](double n) { return r.cols ? n * page : ceil(n / 4.0) * page; };  // n pages
     const double even = work((double)pages * heads / room);                         // all of it, spread evenly
     double least = kRequest * ((s.n_requests * heads + room - 1) / room) + (work((double)most_pages) > even ? work((double)most_pages) : even);

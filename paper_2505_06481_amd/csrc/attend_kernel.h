@@ -137,7 +137,7 @@ struct AttendPlan {
 
 // Waves to a SIMD: two where the accumulators and the operands in flight leave half of the registers.
 template <int D, int KIND, int NC>
-constexpr int attend_waves() { return NC == 1 && D <= 128 ? 2 : 1; }
+constexpr int attend_waves() { return (NC == 1 && D <= 128) || (NC == 2 && D == 64) ? 2 : 1; }
 
 template <int D, int KIND, int NC, bool COLS>
 __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_kernel(AttendArgs g)
