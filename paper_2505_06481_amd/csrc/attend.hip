@@ -84,27 +84,31 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 static Shares shares_of(const mmoe_attend_shape& s)
 {
     Shares r;
-    const int G = s.heads / s.cache.kv_heads, most = s.cache.head_dim > 128 ? 2 : 4;
+    const int G = s.heads / s.cache.kv_heads;
     const int64_t C = (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * G;
-    r.cols = C > 16 * most;
-    const int64_t per = r.cols ? (C + 3) / 4 : C;
-    r.nc = !r.cols && per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : per <= 48 ? 3 : 4;
-    if (r.cols && s.cache.head_dim == 64) r.nc = 2;
-    const int wide = 16 * r.nc * (r.cols ? 4 : 1);
-    r.groups = (int)((C + wide - 1) / wide);
     const int64_t cap = (int64_t)s.max_pages * kPage;
     const int64_t longest = s.max_keys && s.max_keys < cap ? s.max_keys : cap;
     const int64_t sum = s.sum_keys ? s.sum_keys : (int64_t)s.n_requests * longest;
     const int64_t pages = sum / kPage + s.n_requests, most_pages = (longest + kPage - 1) / kPage;
+    // 32 columns to a wavefront leave room for a second one on its SIMD, whose vector instructions run under the first one's matrix
+    // instructions.  33 to 48 columns are two sets of them, or, with long contexts, three tiles to a lone wavefront, which reads the keys
+    // once.  Two sets : three tiles, us: 11 requests of 10 tokens over 2900 keys, int8, 40 columns 27.7 : 32.0; 32 over 6000 71.9 : 80.0 (46
+    // pages to a compute unit); 7 over 11000 38.8 : 46.2; but 8 over 60000, 48 columns (234 pages) fp8 246 : 199, int8 257 : 201,
+    // bf16 (30000) 196 : 188, fp32 (15000) 311 : 252, heads of 64, fp8 137 : 129.  (64 columns so: fp8 233 : 224, bf16 205 : 228.)
+    const bool three = C > 32 && C <= 48 && s.cache.head_dim <= 128 && pages * s.cache.kv_heads >= 100 * 256;
+    r.nc = C <= 16 ? 1 : three ? 3 : 2;
+    r.sets = C <= 32 || three ? 1 : C <= 64 ? 2 : 4;
+    const int wide = 16 * r.nc * r.sets;
+    r.groups = (int)((C + wide - 1) / wide);
     // Estimated cycles: a page to a wavefront (its memory share and NC times the work on 16 columns), a request that a workgroup
-    // takes up, and the join (more where a request has many parts).  Wavefronts with different keys take four pages at once.
+    // takes up, and the join (more where a request has many parts).  Wavefronts with different keys take pages at once.
     const double wide_heads = s.cache.head_dim / 128.0;
     const double page = s.cache.format != MMOE_CACHE_PLAIN ? 2000.0 + 1500.0 * r.nc * wide_heads
                         : s.cache.dtype == MMOE_BF16       ? 2500.0 + 1400.0 * r.nc * wide_heads
                                                            : 3000.0 + 8500.0 * r.nc * wide_heads;
     constexpr double kRequest = 12000.0, kJoin = 14000.0;
-    const int64_t room = 256 * ((r.nc == 1 && s.cache.head_dim <= 128) || (r.nc == 2 && s.cache.head_dim == 64) ? 2 : 1), heads = (int64_t)s.cache.kv_heads * r.groups;
-    auto work = [&](double n) { return r.cols ? n * page : ceil(n / 4.0) * page; };  // n pages
+    const int64_t room = s.cache.head_dim <= 128 && !three ? 512 : 256, heads = (int64_t)s.cache.kv_heads * r.groups;
+    auto work = [&](double n) { return ceil(n * r.sets / 4.0) * page; };  // n pages
     const double even = work((double)pages * heads / room);                         // all of it, spread evenly
     double least = kRequest * ((s.n_requests * heads + room - 1) / room) + (work((double)most_pages) > even ? work((double)most_pages) : even);
     r.shares = 0;

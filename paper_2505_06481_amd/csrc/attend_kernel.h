@@ -18,14 +18,13 @@ namespace mmoe {
 
 enum { kBf16 = 0, kInt8 = 1, kFp8 = 2, kF32 = 3 };  // what pages hold
 
-// How a call is shared out: 16-column tiles to a wavefront, whether the wavefronts of a workgroup take different columns or
-// different keys, groups of columns, and workgroups for each key head and column group: one for each request (shares 0), or
+// How a call is shared out: 16-column tiles to a wavefront; sets of columns to a workgroup's four wavefronts, which take different
+// keys within a set; groups of columns; and workgroups for each key head and column group: one for each request (shares 0), or
 // `shares` ones that take equal parts of all requests' pages one after the other.
 struct Shares {
-    int nc, groups, shares;
-    bool cols;
+    int nc, sets, groups, shares;
 };
-constexpr int kMaxShared = 4096;  // requests whose pages are shared out
+constexpr int kMaxShared = 2048;  // requests whose pages are shared out
 
 // The request's drafted tokens, its keys, and their pages.
 struct Request {
@@ -137,9 +136,9 @@ struct AttendPlan {
 
 // Waves to a SIMD: two where the accumulators and the operands in flight leave half of the registers.
 template <int D, int KIND, int NC>
-constexpr int attend_waves() { return (NC == 1 && D <= 128) || (NC == 2 && D == 64) ? 2 : 1; }
+constexpr int attend_waves() { return (NC == 1 && D <= 128) || (NC == 2 && D <= 128) ? 2 : 1; }
 
-template <int D, int KIND, int NC, bool COLS>
+template <int D, int KIND, int NC, int CW>
 __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_kernel(AttendArgs g)
 {
     using L = AttendPlan<D, KIND, NC>;
@@ -164,11 +163,13 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     const int share = id;
     if (share >= (g.shares ? g.shares : g.B)) return;  // uniform
 
-    constexpr int kQWaves = COLS ? 4 : 1;  // wavefronts with the same columns share them
-    constexpr int kQBytes = L::kLdsQ ? kQWaves * NC * QS * 1024 : 16;
-    constexpr int kRow = 36, kSumBytes = COLS ? 16 : 2 * 4 * 16 * NC * kRow * 4;
+    // CW sets of columns, each for KW wavefronts that share its queries and take different keys
+    constexpr int KW = 4 / CW, kWide = CW * 16 * NC;
+    constexpr int kQBytes = L::kLdsQ ? CW * NC * QS * 1024 : 16;
+    constexpr int kRow = 36, kSumBytes = KW == 1 ? 16 : 2 * KW * kWide * kRow * 4;
+    const int set = wave % CW, turn = wave / CW;
     __shared__ __attribute__((aligned(16))) char lds[kQBytes > kSumBytes ? kQBytes : kSumBytes];  // queries, and at the end the join's sums
-    __shared__ float mls[COLS ? 1 : 4][16 * NC][2];
+    __shared__ float mls[KW == 1 ? 1 : KW][kWide][2];
     __shared__ int first_page[kMaxShared + 1];  // of each request among all pages (fewer than 2^30, or there are no shares)
 
     int at = 0, until = 1;  // pages of the share
@@ -217,7 +218,6 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
     tid = fresh(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const Request r = request_of(g, b);
     const int start = r.start, n = r.n, ctx = r.ctx, total = r.total, C = n * g.G;
-    constexpr int kWide = COLS ? 64 * NC : 16 * NC;
     // pages of the request that are the share's; `slot`: where its part goes, -1 if it is all of the request
     int page0 = 0, page1 = r.pages, slot = -1;
     if (g.shares) {
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         at = until;
     }
     if (cg * kWide >= C) continue;  // uniform
-    const int col0 = cg * kWide + (COLS ? wave * 16 * NC : 0);
+    const int col0 = cg * kWide + set * 16 * NC;
 
     // what the last column of these sees at most
     const int last_token = min(C - 1, cg * kWide + kWide - 1) / g.G;
@@ -252,6 +252,8 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             constexpr int i = decltype(x)::value;
             kf[i / NKS][i % NKS] = *(const u32x4*)(src + i * 1024);
         });
+    };
+    auto load_ks = [&](int64_t block) {
         if constexpr (kCodes)
             each<KT>([&](auto x) { ks[decltype(x)::value] = *(const f32x4*)(g.k_scale + block * kPage + lg * 4 + decltype(x)::value * 16); });
     };
@@ -264,21 +266,25 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         if constexpr (kCodes)
             each<KT>([&](auto x) { vs[decltype(x)::value] = *(const f32x4*)(g.v_scale + block * kPage + lg * 4 + decltype(x)::value * 16); });
     };
-    constexpr int kStride = COLS ? 1 : 4;
-    int step = step0 + (COLS ? 0 : wave);
-    const bool works = step < step1 && (!COLS || col0 < C);  // uniform over the wavefront
+    constexpr int kStride = KW;
+    constexpr bool kLate = attend_waves<D, KIND, NC>() == 2 && NC == 2 && D == 128;
+    int step = step0 + turn;
+    const bool works = step < step1 && col0 < C;  // uniform over the wavefront
     int page = 0;
     if (works) {
         page = page_of(step);
         const int64_t block = block_of(page);
         load_k(block, step);
-        load_vs(block);
-        each<DT>([&](auto dt) { load_v(block, step, dt); });
+        if constexpr (!kLate) {
+            load_ks(block);
+            load_vs(block);
+            each<DT>([&](auto dt) { load_v(block, step, dt); });
+        }
     }
 
     // ---- queries ----
-    if constexpr (L::kLdsQ || !COLS) __syncthreads();  // the request before is done with the LDS
-    char* const lds_q = lds + (COLS ? wave * NC * QS * 1024 : 0) + lane * 16;
+    if constexpr (L::kLdsQ || KW > 1) __syncthreads();  // the request before is done with the LDS
+    char* const lds_q = lds + set * NC * QS * 1024 + lane * 16;
     u32x4 q_reg[L::kLdsQ ? 1 : QS];
     float mult[NC];  // of the scores, in base 2; positive
     int token[NC];   // of the request; n where the column is none
@@ -317,7 +323,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         each<QS>([&](auto x) {
             constexpr int i = decltype(x)::value;
             if constexpr (!L::kLdsQ) q_reg[i] = q[i];
-            else if (COLS || wave == ct % 4) *(u32x4*)(lds_q + (ct * QS + i) * 1024) = q[i];
+            else if (turn == ct % KW) *(u32x4*)(lds_q + (ct * QS + i) * 1024) = q[i];
         });
     });
     if constexpr (L::kLdsQ) __syncthreads();
@@ -359,6 +365,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         const int there = hole ? 0 : total;  // keys from here on are not seen by anybody
         const int left = there - key0 - lg * 4;  // those of them from the lane's first key on
 
+        if constexpr (kLate) load_ks(block_of(page));
         f32x4 s[NC][KT];
         each<NC * KT>([&](auto x) { s[decltype(x)::value / KT][decltype(x)::value % KT] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
         u32x4 q_now[NC], q_next[NC];
@@ -390,6 +397,12 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             if constexpr (NC > 1) __builtin_amdgcn_sched_barrier(0);  // (the compiler would fetch all queries first)
         });
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kLate) {
+            const int64_t block = block_of(page);
+            load_vs(block);
+            each<DT>([&](auto dt) { load_v(block, step, dt); });
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if constexpr (kCodes) {
             each<KT>([&](auto ktc) {
                 constexpr int kt = decltype(ktc)::value;
@@ -417,6 +430,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             each<KT>([&](auto kt) { vs[decltype(kt)::value] *= up; });
         }
         load_k(next_block, ahead);
+        if constexpr (!kLate) load_ks(next_block);
         __builtin_amdgcn_sched_barrier(0);
 
         u32x4 p[NC][NP];
@@ -567,7 +581,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             }
             each<NC>([&](auto ct) { pin(decltype(ct)::value); });
         }
-        load_vs(next_block);
+        if constexpr (!kLate) load_vs(next_block);
         each<DT>([&](auto dtc) {
             constexpr int dt = decltype(dtc)::value;
             if constexpr (kCodes) {
@@ -583,7 +597,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             }
         });
         __builtin_amdgcn_sched_barrier(0);
-        each<DT>([&](auto dt) { load_v(next_block, ahead, dt); });
+        if constexpr (!kLate) each<DT>([&](auto dt) { load_v(next_block, ahead, dt); });
         __builtin_amdgcn_sched_barrier(0);
         step = next;
         page = next_page;
@@ -620,7 +634,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         }
     };
     auto share_of = [&](float ll) { return !direct ? 1.0f : ll != 0.0f ? 1.0f / ll : 0.0f; };  // partial results stay sums
-    if constexpr (COLS) {
+    if constexpr (KW == 1) {
         each<NC>([&](auto ctc) {
             constexpr int ct = decltype(ctc)::value;
             const int c = col0 + ct * 16 + lr;
@@ -632,52 +646,53 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             }
         });
     } else {
-        // The four wavefronts had different keys: join them, 32 elements of the columns at a time, in two buffers in turn.
-        float(*sums)[4][16 * NC][kRow] = (float(*)[4][16 * NC][kRow])lds;
+        // Wavefronts with the same columns had different keys: join them, 32 elements of the columns at a time, in two buffers in turn.
+        float(*sums)[KW][kWide][kRow] = (float(*)[KW][kWide][kRow])lds;
+        const int first = cg * kWide;  // column of the workgroup
         each<NC>([&](auto ctc) {
             constexpr int ct = decltype(ctc)::value;
             if (lg == 0) {
-                mls[wave][ct * 16 + lr][0] = m[ct];
-                mls[wave][ct * 16 + lr][1] = l[ct];
+                mls[turn][set * 16 * NC + ct * 16 + lr][0] = m[ct];
+                mls[turn][set * 16 * NC + ct * 16 + lr][1] = l[ct];
             }
         });
         __syncthreads();
-        if (tid < 16 * NC) {
-            float top = -INFINITY, ll = 0.0f, f[4];
+        if (tid < kWide) {
+            float top = -INFINITY, ll = 0.0f, f[KW];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, mls[w][tid][0]);
+            for (int w = 0; w < KW; ++w) top = fmaxf(top, mls[w][tid][0]);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < KW; ++w) {
                 f[w] = pow2(mls[w][tid][0] - (top == -INFINITY ? 0.0f : top));
                 ll += mls[w][tid][1] * f[w];
             }
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mls[w][tid][0] = f[w] * share_of(ll);
-            if (col0 + tid < C) put_sums(col0 + tid, top, ll);
+            for (int w = 0; w < KW; ++w) mls[w][tid][0] = f[w] * share_of(ll);
+            if (first + tid < C) put_sums(first + tid, top, ll);
         }
         __syncthreads();
-        constexpr int kPer = (16 * NC * 8 + 255) / 256;  // of a thread: four elements of a column
+        constexpr int kPer = (kWide * 8 + 255) / 256;  // of a thread: four elements of a column
         int64_t to[kPer];
         each<kPer>([&](auto x) {
             const int c = (tid + decltype(x)::value * 256) / 8;
-            to[decltype(x)::value] = place(min(col0 + c, C - 1));
+            to[decltype(x)::value] = place(min(first + c, C - 1));
         });
         float f[NC];
-        each<NC>([&](auto ct) { f[decltype(ct)::value] = mls[wave][decltype(ct)::value * 16 + lr][0]; });
+        each<NC>([&](auto ct) { f[decltype(ct)::value] = mls[turn][set * 16 * NC + decltype(ct)::value * 16 + lr][0]; });
         each<D / 32>([&](auto passc) {
             constexpr int pass = decltype(passc)::value, buf = pass & 1;
             each<NC * 2>([&](auto x) {
                 constexpr int ct = decltype(x)::value / 2, i = decltype(x)::value % 2;
-                *(f32x4*)&sums[buf][wave][ct * 16 + lr][i * 16 + lg * 4] = o[ct][pass * 2 + i] * f[ct];
+                *(f32x4*)&sums[buf][turn][set * 16 * NC + ct * 16 + lr][i * 16 + lg * 4] = o[ct][pass * 2 + i] * f[ct];
             });
             __syncthreads();
             each<kPer>([&](auto xc) {
                 const int i = tid + decltype(xc)::value * 256, c = i / 8, d = i % 8 * 4;
-                if (c < 16 * NC && col0 + c < C) {
+                if (c < kWide && first + c < C) {
                     f32x4 x = *(f32x4*)&sums[buf][0][c][d];
 #pragma unroll
-                    for (int w = 1; w < 4; ++w) x += *(f32x4*)&sums[buf][w][c][d];
-                    put(col0 + c, to[decltype(xc)::value], pass * 32 + d, x);
+                    for (int w = 1; w < KW; ++w) x += *(f32x4*)&sums[buf][w][c][d];
+                    put(first + c, to[decltype(xc)::value], pass * 32 + d, x);
                 }
             });
         });
@@ -691,14 +706,11 @@ static void attend_wide(const Shares& r, const AttendArgs& g, hipStream_t st)
     const int64_t sets = ((int64_t)g.kv_heads * (r.shares ? r.shares : g.B) + 7) / 8 * 8;
     const dim3 grid((unsigned)(sets * r.groups)), block(256);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
-    if (r.cols) {
-        if constexpr (D <= 128) r.nc == 2 ? go(attend_kernel<D, KIND, 2, true>) : r.nc == 3 ? go(attend_kernel<D, KIND, 3, true>) : go(attend_kernel<D, KIND, 4, true>);
-        else go(attend_kernel<D, KIND, 2, true>);
-    } else {
-        if (r.nc == 1) go(attend_kernel<D, KIND, 1, false>);
-        else if (r.nc == 2) go(attend_kernel<D, KIND, 2, false>);
-        else if constexpr (D <= 128) r.nc == 3 ? go(attend_kernel<D, KIND, 3, false>) : go(attend_kernel<D, KIND, 4, false>);
-    }
+    if (r.sets == 1) {
+        if (r.nc == 1) go(attend_kernel<D, KIND, 1, 1>);
+        else if (r.nc == 2) go(attend_kernel<D, KIND, 2, 1>);
+        else if constexpr (D <= 128) go(attend_kernel<D, KIND, 3, 1>);
+    } else r.sets == 2 ? go(attend_kernel<D, KIND, 2, 2>) : go(attend_kernel<D, KIND, 2, 4>);
 }
 
 template <int KIND>
