@@ -108,13 +108,15 @@ static Shares shares_of(const mmoe_attend_shape& s)
                                                            : 3000.0 + 8500.0 * r.nc * wide_heads;
     constexpr double kRequest = 12000.0, kJoin = 14000.0;
     const int64_t room = s.cache.head_dim <= 128 && !three ? 512 : 256, heads = (int64_t)s.cache.kv_heads * r.groups;
-    auto work = [&](double n) { return ceil(n * r.sets / 4.0) * page; };  // n pages
+    const int kept = s.cache.head_dim * (s.cache.format != MMOE_CACHE_PLAIN ? 1 : (int)elem_size(s.cache.dtype));
+    const double steps = s.cache.format != MMOE_CACHE_PLAIN || kept <= 128 ? 1.0 : kept <= 256 || s.cache.dtype == MMOE_BF16 ? 2.0 : 4.0;  // to a page
+    auto work = [&](double n) { return ceil(n * steps * r.sets / 4.0) * page / steps; };  // n pages
     const double even = work((double)pages * heads / room);                         // all of it, spread evenly
     double least = kRequest * ((s.n_requests * heads + room - 1) / room) + (work((double)most_pages) > even ? work((double)most_pages) : even);
     r.shares = 0;
     if (s.n_requests <= kMaxShared && s.n_requests * (int64_t)s.max_pages < (int64_t)1 << 30) {
         // rounds of resident workgroups, or shares of a few pages
-        const int64_t tries[] = {room / heads, 2 * room / heads, 3 * room / heads, 4 * room / heads, pages / 4, pages / 8, pages / 16, pages / 32};
+        const int64_t tries[] = {room / heads, 2 * room / heads, 3 * room / heads, 4 * room / heads, pages, pages / 2, pages / 4, pages / 8, pages / 16, pages / 32};
         for (int64_t w : tries) {
             if (w < 2 || w > kMaxShares || w > pages) continue;
             const double each = (double)pages / w, taken = 1.0 + (double)s.n_requests / w;  // pages, requests of a share
