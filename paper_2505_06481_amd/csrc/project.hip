@@ -56,32 +56,50 @@ struct ShrinkArgs {
     int T, K, R, Rp, n;
     int chunk;        // tokens
     int groups;       // of a chunk
+    int pairs;        // of blocks of 16 ranks: a workgroup takes one
     bool by_token;    // groups are tokens (chunks of up to kScan)
 };
 constexpr int kScan = 512;  // tokens looked through at once
+struct TokenList {
+    int list[kScan];
+    int counts[4];
+};
 struct ShrinkLds {
     float part[4][32][33];
-    int list[kScan];
-    int count;
+    TokenList tokens;
 };
 
 // The tokens t0 .. t0 + count - 1 (at most kScan) with adapter a, ascending, to `list`; returns how many.  a = n stands for none.
-__device__ __forceinline__ int tokens_of(const int32_t* aid, int t0, int count, int a, int n, int* list, int* shared_count)
+__device__ __forceinline__ int tokens_of(const int32_t* aid, int t0, int count, int a, int n, TokenList& l)
 {
-    // one wavefront: 64 at a time, in order
-    if (threadIdx.x < 64) {
-        int at = 0;
-        for (int i = threadIdx.x; i < (count + 63) / 64 * 64; i += 64) {
-            const int x = n && i < count ? aid[t0 + i] : -1;
-            const bool mine = i < count && ((unsigned)x < (unsigned)n ? x == a : a == n);
-            const uint64_t who = __ballot(mine);
-            if (mine) list[at + __popcll(who & (((uint64_t)1 << threadIdx.x) - 1))] = t0 + i;
-            at += __popcll(who);
-        }
-        if (threadIdx.x == 0) *shared_count = at;
+    constexpr int kPer = kScan / 256;  // runs of 64 tokens of a wavefront
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t who[kPer];
+    bool mine[kPer];
+    int have = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int at = (wave * kPer + i) * 64 + lane;
+        const int x = n && at < count ? aid[t0 + at] : -1;
+        mine[i] = at < count && ((unsigned)x < (unsigned)n ? x == a : a == n);
+        who[i] = __ballot(mine[i]);
+        have += __popcll(who[i]);
+    }
+    if (lane == 0) l.counts[wave] = have;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += l.counts[w];
+        all += l.counts[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (mine[i]) l.list[before + __popcll(who[i] & (((uint64_t)1 << lane) - 1))] = t0 + (wave * kPer + i) * 64 + lane;
+        before += __popcll(who[i]);
     }
     __syncthreads();
-    return __builtin_amdgcn_readfirstlane(*shared_count);
+    return __builtin_amdgcn_readfirstlane(all);
 }
 
 // The adapter of a group (n: none), or -1 if the group has no tokens to look for.
@@ -106,7 +124,7 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
     const int slices = g.K * kEsz / 64, per = slices / 4;  // 64 bytes of a row each
     const char* x[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) x[j] = g.X + (int64_t)lds.list[at + min(j * 16 + lr, count - 1)] * g.ldx * kEsz + wave * per * 64 + lg * 16;
+    for (int j = 0; j < 2; ++j) x[j] = g.X + (int64_t)lds.tokens.list[at + min(j * 16 + lr, count - 1)] * g.ldx * kEsz + wave * per * 64 + lg * 16;
     const char* w = g.Ap + (((int64_t)a * (g.Rp / 16) + rb0) * slices + wave * per) * 1024 + lane * 16;
     f32x4 acc[RB][2];
 #pragma unroll
@@ -134,7 +152,8 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
     };
     int s = 0;
     for (; s + 8 <= per; s += 8) slice(std::integral_constant<int, 8>{}, s);
-    for (; s < per; s += 2) slice(std::integral_constant<int, 2>{}, s);  // (K is a multiple of 256, eight slices: per is even)
+    if (s + 4 <= per) slice(std::integral_constant<int, 4>{}, s), s += 4;
+    if (s < per) slice(std::integral_constant<int, 2>{}, s);  // (K is a multiple of 256, eight slices: per is even)
     __syncthreads();  // the sums of the tiles before have been read
 #pragma unroll
     for (int i = 0; i < RB; ++i)
@@ -147,7 +166,7 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
     for (int i = tid; i < count * cols; i += 256) {  // cols: those of U from rb0 on; the padding's are zeros
         const int tok = i / cols, r = i % cols;
         const float v = r < RB * 16 ? (lds.part[0][r][tok] + lds.part[1][r][tok] + (lds.part[2][r][tok] + lds.part[3][r][tok])) * f : 0.0f;
-        const int64_t to = (int64_t)lds.list[at + tok] * g.Rp * kParts + rb0 * 16 + r;
+        const int64_t to = (int64_t)lds.tokens.list[at + tok] * g.Rp * kParts + rb0 * 16 + r;
         if (F32) {
             ((float*)g.U)[to] = v;
         } else {
@@ -159,21 +178,19 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
 }
 
 template <bool F32>
-__device__ __forceinline__ void shrink_body(const ShrinkArgs& g, ShrinkLds& lds, int group, int chunk)
+__device__ __forceinline__ void shrink_body(const ShrinkArgs& g, ShrinkLds& lds, int group, int chunk, int rb)
 {
     const int t0 = chunk * g.chunk, t1 = min(t0 + g.chunk, g.T);
     const int a = adapter_of(g.aid, t0, t1 - t0, group, g.by_token, g.n);
     if (a < 0 || a >= g.n) return;  // uniform
-    const int real = (g.R + 15) / 16;  // blocks of 16 that hold ranks
+    const int real = (g.R + 15) / 16;                            // blocks of 16 that hold ranks; this workgroup's are rb and rb + 1
+    const int cols = rb + 2 < real ? 32 : g.Rp - rb * 16;
     for (int t = t0; t < t1; t += kScan) {
         __syncthreads();  // the list before has been used
-        const int count = tokens_of(g.aid, t, min(kScan, t1 - t), a, g.n, lds.list, &lds.count);
+        const int count = tokens_of(g.aid, t, min(kScan, t1 - t), a, g.n, lds.tokens);
         for (int at = 0; at < count; at += 32)
-            for (int rb = 0; rb < real; rb += 2) {
-                const int cols = rb + 2 < real ? 32 : g.Rp - rb * 16;
-                if (rb + 1 < real) shrink_tiles<F32, 2>(g, lds, a, rb, cols, at, min(32, count - at));
-                else shrink_tiles<F32, 1>(g, lds, a, rb, cols, at, min(32, count - at));
-            }
+            if (rb + 1 < real) shrink_tiles<F32, 2>(g, lds, a, rb, cols, at, min(32, count - at));
+            else shrink_tiles<F32, 1>(g, lds, a, rb, cols, at, min(32, count - at));
     }
 }
 
@@ -181,7 +198,7 @@ template <bool F32>
 __global__ __launch_bounds__(256) void shrink_kernel(ShrinkArgs g)
 {
     __shared__ ShrinkLds lds;
-    shrink_body<F32>(g, lds, blockIdx.y, blockIdx.x);
+    shrink_body<F32>(g, lds, blockIdx.y, blockIdx.x, blockIdx.z * 2);
 }
 
 // ---- Y = X W + U B -----------------------------------------------------------------------------------
@@ -429,7 +446,10 @@ __global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_
         ShrinkLds shrink;
     } lds;
     if ((int)blockIdx.x < tiles) tile_body<F32, WM, WN>(g, lds.tile, blockIdx.x, tiles);
-    else shrink_body<F32>(u, lds.shrink, (blockIdx.x - tiles) % u.groups, (blockIdx.x - tiles) / u.groups);
+    else {
+        const int id = blockIdx.x - tiles, pair = id % u.pairs, of = id / u.pairs;
+        shrink_body<F32>(u, lds.shrink, of % u.groups, of / u.groups, pair * 2);
+    }
 }
 
 // Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes tokens of one adapter (or of none) among kScan, 16 of
@@ -438,16 +458,16 @@ template <bool F32>
 __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool by_token, int sixteens)
 {
     constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
-    __shared__ int list[kScan], shared_count;
+    __shared__ TokenList tokens;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
     const int t0 = blockIdx.z / sixteens * kScan, some = min(kScan, g.T - t0);
     const int a = adapter_of(g.aid, t0, some, blockIdx.y, by_token, g.n);
     if (a < 0) return;  // uniform
-    const int count = tokens_of(g.aid, t0, some, a, g.n, list, &shared_count);
+    const int count = tokens_of(g.aid, t0, some, a, g.n, tokens);
     const int nb = (blockIdx.x * 4 + wave) * 4, rs = a < g.n ? g.Rp * kEsz / 64 : 0;
     const char* b = g.Bp + ((int64_t)a * (g.N / 16) + nb) * rs * 1024 + lane * 16;
     for (int at = blockIdx.z % sixteens * 16; at < count; at += sixteens * 16) {
-        const int64_t t = list[min(at + lr, count - 1)];
+        const int64_t t = tokens.list[min(at + lr, count - 1)];
         const float* part = g.part + t * g.N + nb * 16 + lg * 4;
         f32x4 acc[4];
 #pragma unroll
@@ -480,6 +500,7 @@ __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool b
 // Few tokens run in two launches: parts of X W beside U, then their join with U B.  More in two as well: U, then tiles
 // that add U B themselves.
 constexpr int kFewTokens = 4096;
+static int shrink_chunk(int n, int most) { return 32 * n < most ? 32 * n : most; }
 struct ProjectPlan {
     int wm, wn, splits;
     bool few;
@@ -494,24 +515,27 @@ static ProjectPlan project_plan(const mmoe_project_shape& s)
         double alone, two, ends;  // cycles of a step; of one of each of two; of a tile's beginning and end
     };
     static const Tile tiles[] = {{8, 8, 1450.0, 0.0, 25000.0}, {4, 8, 900.0, 1800.0, 15000.0}, {4, 4, 680.0, 1430.0, 6000.0}, {2, 4, 440.0, 0.0, 4000.0}};
-    constexpr double kLaunch = 7000.0, kBytes = 1200.0;  // a launch more; bytes of parts a cycle
+    constexpr double kLaunch = 7000.0, kBytes = 1200.0, kRound = 10000.0;  // a launch more; bytes of parts a cycle; a round of making U
     const bool f32 = s.dtype == MMOE_F32;
     const int slices = s.d_in / (f32 ? 16 : 32);
     const int T = (s.T + 31) / 32 * 32, most = s.T > kFewTokens ? 0 : s.d_in / 256 < 16 ? s.d_in / 256 : 16;
+    const int chunk = s.n_adapters ? shrink_chunk(s.n_adapters, kScan) : kScan;
     ProjectPlan best = {8, 8, 1, false};
     double least = 1e30;
     for (const Tile& t : tiles) {
         const int64_t n = (int64_t)((T + 32 * t.wm - 1) / (32 * t.wm)) * (s.d_out / (32 * t.wn));
         const double matrix = f32 ? t.wm * t.wn * 135.0 : 0.0;
         for (int splits = 0; splits <= most; ++splits) {  // 0: not in parts
-            // beside the parts run the workgroups that make U
-            const int64_t wgs = splits ? n * splits + (s.n_adapters < T ? s.n_adapters : T) * ((T + kScan - 1) / kScan) : n, room = t.two > 0.0 ? 512 : 256, full = wgs / room, rest = wgs % room;
+            const int64_t wgs = splits ? n * splits : n, room = t.two > 0.0 ? 512 : 256, full = wgs / room, rest = wgs % room;
             const double steps = (double)slices / (splits ? splits : 1);
             const double alone = (t.alone > matrix ? t.alone : matrix) * steps + t.ends;
             const double two = (t.two > 2.0 * matrix ? t.two : 2.0 * matrix) * steps + t.ends;
             double time = full * (room == 512 ? two : alone) + (rest > 256 ? two : rest ? alone : 0.0);
+            // beside the parts run the workgroups that make U, in a round of their own where the last round has no room for them
+            const int64_t beside = splits && s.n_adapters ? (s.n_adapters < T ? s.n_adapters : T) * ((T + chunk - 1) / chunk) * ((s.rank + 31) / 32) : 0;
+            if (beside && (rest ? rest : room) + beside > room) time += kRound * (((rest ? rest : room) + beside - 1) / room);
             if (splits) time += kLaunch + (2.0 * splits + 1.0) * T * s.d_out * 4.0 / kBytes;
-            else if (s.n_adapters) time += 2.5 * kLaunch + 700.0 * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
+            else if (s.n_adapters) time += 2.5 * kLaunch + 1500.0 * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
             if (time < least) least = time, best = {t.wm, t.wn, splits ? splits : 1, splits > 0};
         }
     }
@@ -552,16 +576,17 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
     const ProjectPlan p = project_plan(s);
     ProjectArgs g = {(const char*)X, (const char*)Wp, (const char*)Bp, (const char*)ws, (char*)Y, p.few ? (float*)((char*)ws + u_bytes(s)) : nullptr, aid,
                      ldx, ldy, s.T, s.d_in, s.d_out, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
-    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, n, false};
+    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, n, (s.rank + 31) / 32, false};
     const int tiles = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
     const dim3 block(256);
     if (p.few) {
         const int chunk = s.T < kScan ? s.T : kScan, chunks = (s.T + kScan - 1) / kScan;
         const bool by_token = n + 1 > chunk;
         u.by_token = by_token;
-        u.chunk = chunk;
+        // U: about 32 tokens of an adapter to a workgroup, so that it is done before the tiles are
+        u.chunk = by_token ? chunk : shrink_chunk(n, chunk);
         u.groups = by_token ? chunk : n;
-        const dim3 grid(tiles + (n ? u.groups * chunks : 0));
+        const dim3 grid(tiles + (n ? u.groups * u.pairs * ((s.T + u.chunk - 1) / u.chunk) : 0));
         auto parts = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g, u, tiles); };
         if (p.wm == 8) parts(project_parts_kernel<F32, 8, 8>);
         else if (p.wn == 8) parts(project_parts_kernel<F32, 4, 8>);
@@ -577,7 +602,7 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
         const int chunks = n >= 512 ? 1 : 512 / n;
         u.chunk = (s.T + chunks - 1) / chunks;
         if (u.chunk < 32) u.chunk = 32;
-        hipLaunchKernelGGL(shrink_kernel<F32>, dim3((s.T + u.chunk - 1) / u.chunk, n), block, 0, st, u);
+        hipLaunchKernelGGL(shrink_kernel<F32>, dim3((s.T + u.chunk - 1) / u.chunk, n, u.pairs), block, 0, st, u);
     }
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles), block, 0, st, g); };
     if (p.wm == 8) go(project_tile_kernel<F32, 8, 8>);
