@@ -172,7 +172,8 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
         } else {
             const uint16_t hi = f32_to_bf16_bits(v);
             ((uint16_t*)g.U)[to] = hi;
-            ((uint16_t*)g.U)[to + g.Rp] = f32_to_bf16_bits(v - bf16_bits_to_f32(hi));
+            const float left = v - bf16_bits_to_f32(hi);  // NaN where v is not finite: then the rounded value is all
+            ((uint16_t*)g.U)[to + g.Rp] = f32_to_bf16_bits(left == left ? left : 0.0f);
         }
     }
 }
@@ -231,7 +232,46 @@ struct TileLds {
     static constexpr int kStages = WM == 2 ? 8 : WM == 4 && WN == 8 ? 3 : 4;
     __attribute__((aligned(1024))) char ring[kStages * kStep];
     uint32_t used[kMaxAdapters / 32];
+    uint32_t odd[4][kMaxAdapters / 32];  // adapters with infinities or NaN among a wavefront's features
 };
+
+// Adds to a wavefront's part of Y what the adapters in `odd` give: 64 bytes of rank at a time, those that are not finite.
+// Tokens t0 .., blocks of 16 features from f0 on.
+template <bool F32, int WM, int WN>
+__device__ __forceinline__ void add_odd(const ProjectArgs& g, const uint32_t* odd, int t0, int f0)
+{
+    constexpr int kEsz = F32 ? 4 : 2, kParts = F32 ? 1 : 2;
+    int lane = threadIdx.x & 63;
+    asm("" : "+v"(lane));  // nothing of this is worked out ahead
+    const int lr = lane & 15, lg = lane >> 4, rs = g.Rp * kEsz / 64;
+    __threadfence_block();  // other lanes wrote Y
+    for (int word = 0; word < (g.n + 31) / 32; ++word)
+        for (uint32_t bits = __builtin_amdgcn_readfirstlane(odd[word]); bits; bits &= bits - 1) {
+            const int a = word * 32 + __ffs(bits) - 1;
+            const char* b = g.Bp + ((int64_t)a * (g.N / 16) + f0) * rs * 1024 + lane * 16;
+#pragma unroll 1
+            for (int x = 0; x < WM * WN; ++x) {
+                const int j = x / WN, i = x % WN, t = min(t0 + j * 16 + lr, g.T - 1);
+                f32x4 own = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+                for (int s = 0; s < rs; ++s) {
+                    f32x4 zero = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int o = 0; o < WN; ++o) zero = mma<F32>(*(const u32x4*)(b + ((int64_t)o * rs + s) * 1024), u32x4{0, 0, 0, 0}, zero);
+                    if (!__any(zero[0] + zero[1] + zero[2] + zero[3] != 0.0f)) continue;  // is in Y
+                    const char* u = g.U + (int64_t)t * kParts * g.Rp * kEsz + s * 64 + lg * 16;
+                    for (int p = 0; p < kParts; ++p)
+                        own = mma<F32>(*(const u32x4*)(b + ((int64_t)i * rs + s) * 1024), *(const u32x4*)(u + p * g.Rp * kEsz), own);
+                }
+                if (t0 + j * 16 + lr < g.T && g.aid[t] == a)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t at = t * g.ldy + (f0 + i) * 16 + lg * 4 + e;
+                        if (F32) ((float*)g.Y)[at] += own[e];
+                        else ((uint16_t*)g.Y)[at] = f32_to_bf16_bits(bf16_bits_to_f32(((uint16_t*)g.Y)[at]) + own[e]);
+                    }
+            }
+        }
+}
 
 template <bool F32, int WM, int WN>
 __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>& shared, int block, int blocks)
@@ -303,6 +343,7 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
     auto arrived = [](const u32x4& f) { asm volatile("" ::"v"(f)); };
     if (g.n && !g.part) {  // adapters of the tile's tokens
         if (tid < kMaxAdapters / 32) used[tid] = 0;
+        if (lane < kMaxAdapters / 32) shared.odd[wave][lane] = 0;
         __syncthreads();
         for (int t = t0 + tid; t < min(t0 + 32 * WM, g.T); t += 256) {
             const int a = g.aid[t];
@@ -348,6 +389,8 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
 
     // Adapters that the tile's tokens use, one by one: tokens of other adapters with zeros, fragments without any not at all.  A token's
     // U is its own adapter's, read once; the weights of the next adapter are on their way while this one's are multiplied.
+    // Zeros keep other tokens apart where the weights are finite; 64 bytes of rank that are not are left for the end (`odd`).
+    bool odd = false;
     if (g.n && !g.part) {
         const int rs = g.Rp * kEsz / 64;
         int mine[WM];
@@ -377,8 +420,16 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
             if (a >= 0) fetch(a);
             while (a >= 0) {
                 each<WN>([&](auto i) { wf[decltype(i)::value] = ahead[decltype(i)::value]; });
+                f32x4 zero = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                each<WN>([&](auto i) { zero = mma<F32>(wf[decltype(i)::value], u32x4{0, 0, 0, 0}, zero); });
                 const int then = next();
                 fetch(then);
+                if (__any(zero[0] + zero[1] + zero[2] + zero[3] != 0.0f)) {
+                    if (lane == 0) shared.odd[wave][a >> 5] |= 1u << (a & 31);
+                    odd = true;
+                    a = then;
+                    continue;
+                }
                 each<WM>([&](auto jc) {
                     constexpr int j = decltype(jc)::value;
                     if (!__any(mine[j] == a)) return;  // uniform
@@ -428,6 +479,7 @@ __device__ __forceinline__ void tile_body(const ProjectArgs& g, TileLds<WM, WN>&
         }
         __builtin_amdgcn_sched_barrier(0);
     }
+    if (odd) add_odd<F32, WM, WN>(g, shared.odd[wave], t0 + wm * WM * 16, f0 + wn * WN);
 }
 
 template <bool F32, int WM, int WN>

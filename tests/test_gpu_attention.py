@@ -164,6 +164,41 @@ def test_project_keeps_other_tokens_apart(at):
         assert torch.equal(bad, (aid == 1) | (torch.arange(T) == 5))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,K,N", [(24, 256, 512), (300, 256, 512), (5000, 256, 512), (4200, 256, 4352)])
+def test_project_weights_that_are_not_finite(at, ref, T, K, N, dtype):
+    """Infinities and NaN in one adapter's B reach its own tokens and nobody else."""
+    g = gen_of(8, T)
+    X, W = rand(g, T, K, dtype=dtype), rand(g, K, N, dtype=dtype, scale=1 / 16)
+    A, B = rand(g, 3, K, 8, dtype=dtype, scale=1 / 16), rand(g, 3, 8, N, dtype=dtype)
+    B[1, :, ::2], B[1, 3, 1::2] = math.nan, math.inf
+    aid = torch.arange(T, dtype=torch.int32) % 4
+    aid[64:96] = 1
+    shape = at.make_project_shape(T, K, N, 3, 8, dtype)
+    args = [at.pack_projection(shape, W.cuda()), *at.pack_adapters(shape, A.cuda(), B.cuda()), torch.ones(3, device="cuda")]
+    Y = at.project(shape, X.cuda(), aid.cuda(), *args, at.project_workspace(shape)).cpu()
+    assert torch.equal(torch.isfinite(Y).all(1), aid != 1) and not torch.isfinite(Y[aid == 1]).any()
+    keep = aid != 1
+    B[1] = 0
+    want = ref.project(X[keep][:512], aid[keep][:512], W, A, B, torch.ones(3))
+    tol = 2.0 ** -8 * want.abs() + 2.0 ** -6 * rms(want) if dtype == "bf16" else torch.full_like(want, 2e-5 * rms(want))
+    close(Y[keep][:512], want, tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,n,R", [(513, 300, 20), (1100, 600, 40), (3000, 3, 72), (4097, 1024, 33), (4160, 2, 128), (9000, 5, 16)])
+def test_project_chunks_of_tokens(at, ref, T, n, R, dtype):
+    """Tokens and adapters around the counts at which the work is cut otherwise."""
+    run_project(at, ref, T, 256, 256, n, R, dtype)
+
+
+@pytest.mark.parametrize("T,K,N,n,dtype", [(2048, 2048, 2048, 4, "bf16"), (4096, 1024, 1024, 3, "bf16"), (8200, 512, 8192, 2, "bf16"), (256, 8192, 512, 4, "bf16"),
+                                           (600, 4096, 2048, 3, "f32"), (2000, 2048, 1024, 3, "f32")])
+def test_project_tiles(at, ref, T, K, N, n, dtype):
+    """Products large and oblong enough for each of the tile shapes, whole and in parts of k."""
+    run_project(at, ref, T, K, N, n, 16, dtype, mix="blocks")
+
+
 def test_project_packed_layout(at):
     for dtype, c in (("bf16", 32), ("f32", 16)):
         K, N, n, R = 256, 512, 2, 12
