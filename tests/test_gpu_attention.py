@@ -335,6 +335,28 @@ def test_cache_round_trip(at, ref, T, H, D, start, dtype, format):
         assert torch.equal(got.cpu(), want)
 
 
+@pytest.mark.parametrize("format", ["plain", "int8", "fp8"])
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 128), ("bf16", 256)])
+def test_cache_reads_lists_of_any_order(at, format, dtype, D):
+    """Contexts one after the other, each from its own place on, backwards, repeated, outside: the same rows as one by one."""
+    g = gen_of(26, D)
+    H, n = 3, 9
+    shape = at.make_cache_shape(n, H, D, dtype, format)
+    cache = at.alloc_cache(shape)
+    x = rand(g, 2, n * 64, H, D, dtype=dtype).cuda()
+    at.cache_append(shape, x[0], x[1], torch.arange(n * 64, dtype=torch.int32, device="cuda"), cache)
+    runs = [range(3, 300), range(70, 71), range(130, 200), range(575, 400, -1), range(64, 128), range(-4, 6), range(570, 580), range(0, 63), range(200, 200)]
+    places = torch.tensor([p for r in runs for p in r], dtype=torch.int32).cuda()
+    K, V = at.cache_read(shape, cache, places)
+    ok = (places >= 0) & (places < n * 64)
+    whole = at.cache_read(shape, cache, torch.arange(n * 64, dtype=torch.int32, device="cuda"))
+    for got, all_ in zip((K, V), whole):
+        assert torch.equal(got[ok], all_[places[ok].long()]) and not got[~ok].any()
+    for p in (3, 64, 575):
+        one = at.cache_read(shape, cache, torch.tensor([p], dtype=torch.int32, device="cuda"))
+        assert all(torch.equal(a[0], b[p]) for a, b in zip(one, whole))
+
+
 def test_cache_layout(at):
     """Pages hold what the header says, where it says."""
     H, D, T = 2, 128, 64
@@ -540,6 +562,18 @@ def test_attend_long_contexts_are_split(at, ref, drafts, dtype, format):
 
 
 @pytest.mark.parametrize("dtype,format", KINDS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("drafts", [[1, 1, 1], [9, 12, 0], [16, 3, 11], [40, 1, 17]])
+def test_attend_hints_that_are_too_large(at, ref, drafts, D, dtype, format):
+    """A call shared out for far more keys than there are: shares without pages, and the tiles and joins of long contexts."""
+    g = gen_of(27, drafts[0], D)
+    p = Paged(at, ref, g, [700, 0, 1500], drafts, 8, 2, D, dtype, format)
+    tree = trees(g, drafts)
+    for keys in (10_000, 200_000, 2_000_000):
+        check_attend(at, ref, p, 8, D, dtype, format, tree, max_keys=keys, sum_keys=keys)
+
+
+@pytest.mark.parametrize("dtype,format", KINDS)
 def test_attend_rows_that_see_nothing(at, ref, dtype, format):
     """An empty mask over an empty context; a mask without the token itself; requests without drafts."""
     g = gen_of(17)
@@ -626,6 +660,44 @@ def test_attend_context_longer_than_the_table(at, ref):
                        p.pages[:, :2].contiguous().cuda(), p.cache, at.attend_workspace(shape))
     want, _ = ref.attend(p.Q, p.starts, p.ctx, None, p.keys, p.values, 0.125, limit=128)
     close(out, want, attend_tol("bf16", "plain", p.values, want))
+
+
+def test_half_beyond_32_bits(at, ref):
+    """Rows, pages and values whose offsets pass 2^32 bytes and 2^31 elements."""
+    g = gen_of(28)
+    T, K, N, H, D = 140001, 256, 16384, 128, 128
+    W = rand(g, K, N, dtype="bf16", scale=1 / 16)
+    A, B = rand(g, 2, K, 8, dtype="bf16", scale=1 / 16), rand(g, 2, 8, N, dtype="bf16")
+    X, aid = rand(g, T, K, dtype="bf16").cuda(), torch.arange(T, dtype=torch.int32) % 2
+    shape = at.make_project_shape(T, K, N, 2, 8, "bf16")
+    Y = at.project(shape, X, aid.cuda(), at.pack_projection(shape, W.cuda()), *at.pack_adapters(shape, A.cuda(), B.cuda()),
+                   torch.ones(2, device="cuda"), at.project_workspace(shape))
+    some = torch.tensor([0, 70000, 131071, 131072, T - 300, T - 2, T - 1])
+    want = ref.project(X[some.cuda()].cpu(), aid[some], W, A, B, torch.ones(2))
+    close(Y[some.cuda()], want, 2.0 ** -8 * want.abs() + 2.0 ** -6 * rms(want))
+    heads = Y.view(T, H, D)
+    before = heads[some.cuda()].clone()
+    steps, m = at.rotary_steps(D)
+    pos = torch.arange(T, dtype=torch.int32).cuda()
+    at.rotary(at.make_rotary_shape(T, H, D, D, "halves", "bf16", m), heads, pos, steps, Y=heads)
+    turned = at.rotary(at.make_rotary_shape(len(some), H, D, D, "halves", "bf16", m), before, pos[some.cuda()].clone(), steps)
+    assert torch.equal(heads[some.cuda()], turned)
+    del Y, heads, X
+    n, ctx = 70000, 200
+    cs = at.make_cache_shape(n, 8, D, "bf16", "plain")  # 9.2 GB of keys
+    cache = at.alloc_cache(cs)
+    pages = torch.tensor([[n - 1, 1, 40000, n - 2]], dtype=torch.int32)
+    k, v = rand(g, ctx + 1, 8, D, dtype="bf16"), rand(g, ctx + 1, 8, D, dtype="bf16")
+    at_ = torch.arange(ctx + 1)
+    places = (pages[0][at_ // 64] * 64 + at_ % 64).to(torch.int32).cuda()
+    at.cache_append(cs, k.cuda(), v.cuda(), places, cache)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(at.cache_read(cs, cache, places), (k, v)))
+    Q = rand(g, 1, 32, D, dtype="bf16")
+    sh = at.make_attend_shape(cs, 1, 1, 32, 4, 1, D ** -0.5)
+    starts, c = torch.tensor([0, 1], dtype=torch.int32), torch.tensor([ctx], dtype=torch.int32)
+    out, _ = at.attend(sh, Q.cuda(), starts.cuda(), c.cuda(), None, pages.cuda(), cache, at.attend_workspace(sh))
+    want, _ = ref.attend(Q, starts, [ctx], None, [k.double()], [v.double()], D ** -0.5)
+    close(out, want, attend_tol("bf16", "plain", [v.double()], want))
 
 
 def test_half_runs_on_another_stream(at, ref):
