@@ -228,8 +228,9 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 template <int WM, int WN>
 struct TileLds {
     static constexpr int kStep = (WM + WN) * 2048;  // bytes of a step: 2 WM token fragments, then 2 WN of weights
-    // steps in the ring: small tiles have as many bytes in flight as large ones; 128 x 256 leaves room for two workgroups
-    static constexpr int kStages = WM == 2 ? 8 : WM == 4 && WN == 8 ? 3 : 4;
+    // steps in the ring: four, but 128 x 256 leaves room for two workgroups (with two 29.5 -> 36.4 us at 2000 x 1024 x 4096; eight of
+    // 64 x 128 fetch more than a short k has: 64 x 256 x 65536 in 21.2 us, with four 16.7)
+    static constexpr int kStages = WM == 4 && WN == 8 ? 3 : 4;
     __attribute__((aligned(1024))) char ring[kStages * kStep];
     uint32_t used[kMaxAdapters / 32];
     uint32_t odd[4][kMaxAdapters / 32];  // adapters with infinities or NaN among a wavefront's features

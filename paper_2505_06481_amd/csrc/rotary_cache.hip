@@ -109,7 +109,9 @@ int launch_rotary(const mmoe_rotary_shape& s, const void* X, const int32_t* pos,
 {
     const int across = 64 / (s.head_dim / 16);
     const int most = (s.heads + across - 1) / across;
-    const int waves = s.T >= 4096 ? 1 : s.T * (int64_t)most <= 8192 ? most : (8192 + s.T - 1) / s.T;
+    // About 4096 wavefronts: fewer leave compute units idle, more make the same sines again.  us, with one to a token, this rule, one to every
+    // `across` heads (48 heads of 128): 64 tokens 5.4, 3.5, 3.5; 512 6.2, 5.3, 5.3; 1024 6.8, 6.9, 7.9; 2048 10.1, 9.9, 12.4; 8192 33.3, 33.3, 37.3.
+    const int waves = s.T * (int64_t)most <= 4096 ? most : s.T < 4096 ? 4096 / s.T : 1;
     const int64_t xh = s.x_head ? s.x_head : s.head_dim, xt = s.x_token ? s.x_token : (int64_t)s.heads * s.head_dim;
     const int64_t yh = s.y_head ? s.y_head : s.head_dim, yt = s.y_token ? s.y_token : (int64_t)s.heads * s.head_dim;
     const dim3 grid((unsigned)(((int64_t)s.T * waves + 3) / 4)), block(256);
@@ -331,13 +333,13 @@ int launch_cache_append(const mmoe_cache_shape& s, const mmoe_cache_rows& rows, 
     return launch_status();
 }
 
-// A wavefront reads the keys or the values of one head and of 64 of the listed places back.  The first of them is chosen so that, where
-// the list starts with a run of places, a wavefront has one page's.
+// A wavefront reads the keys or the values of one head and of `rows` (64, 16 or 4) of the listed places back.  The first of them is
+// chosen so that, where the list starts with a run of places, a wavefront's are one page's.
 template <int FORMAT, bool F32, int D>
 __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, const char* __restrict__ v, const float* __restrict__ ks,
                                                    const float* __restrict__ vs, const int32_t* __restrict__ places,
                                                    char* __restrict__ K, char* __restrict__ V, int R, int heads, int64_t n_places,
-                                                   bool aligned)
+                                                   int rows)
 {
     using P = Kept<FORMAT, F32>;
     constexpr int kEsz = F32 ? 4 : 2, E = P::E;
@@ -346,10 +348,10 @@ __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, c
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int which = (int)(item & 1), h = (int)((item >> 1) % heads);
     const int64_t tile = (item >> 1) / heads;
-    const int64_t r0 = tile * 64 - (aligned ? places[0] & (kPage - 1) : 0);  // first row of the list; rows before 0 and from R on are not there
+    const int64_t r0 = tile * rows - (places[0] & (rows - 1));  // first row of the list; rows before 0 and from R on are not there
     if (r0 >= R) return;  // uniform
     const int64_t mine = r0 + lane;
-    const bool listed = mine >= 0 && mine < R;
+    const bool listed = lane < rows && mine >= 0 && mine < R;
     int p = listed ? places[mine] : -1;
     if (p >= n_places || p < 0) p = -1;
     const uint64_t all = __ballot(listed);
@@ -367,7 +369,7 @@ __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, c
             const int row = part * 16 + (lane & 15);
             const int64_t r = r0 + row;
             const int q = __shfl(p, row);
-            const bool there = r >= 0 && r < R;
+            const bool there = row < rows && r >= 0 && r < R;
             const int64_t ph = (int64_t)(max(q, 0) / kPage) * heads + h;
             const char* base = k + ph * kPage * D * P::kBytes;
             float scale = 1.0f;
@@ -444,13 +446,16 @@ __global__ __launch_bounds__(256) void read_kernel(const char* __restrict__ k, c
 template <int FORMAT, bool F32>
 static void read_back(const mmoe_cache_shape& s, const mmoe_cache& c, int R, const int32_t* places, void* K, void* V, hipStream_t st)
 {
-    // A list of more than a few pages is taken from the page of its first place on; in a short one that look costs a microsecond.
-    const bool aligned = R > 4 * kPage;
-    const int64_t items = ((int64_t)(R + kPage - 1) / 64 + (aligned ? 1 : 0)) * s.kv_heads * 2;
+    // Rows to a wavefront: few of a short list, so that its wavefronts wait at the same time.  us, 8 heads of 128 int8, a run of places | places
+    // apart, with 64, 16 and 4 rows: 64 listed 5.6, 3.9, 3.9 | 51, 15, 5.8; 256 7.0, 4.1, 4.1 | 52, 15, 5.8; 1024 7.5, 4.6, 7.6 | 59, 19, 14;
+    // 4096 9.0, 9.2, 21 | 62, 41, 40; 16384 22.8, 26.1, 72.7 | 195, 187, 175.
+    const int64_t all = (int64_t)R * s.kv_heads;
+    const int rows = all <= 2048 ? 4 : all <= 16384 ? 16 : 64;
+    const int64_t items = ((int64_t)(R + rows - 1) / rows + 1) * s.kv_heads * 2;
     const dim3 grid((unsigned)((items + 3) / 4)), block(256);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, block, 0, st, (const char*)c.k, (const char*)c.v, c.k_scale, c.v_scale, places, (char*)K, (char*)V,
-                           R, s.kv_heads, (int64_t)s.n_pages * kPage, aligned);
+                           R, s.kv_heads, (int64_t)s.n_pages * kPage, rows);
     };
     if (s.head_dim == 64) go(read_kernel<FORMAT, F32, 64>);
     else if (s.head_dim == 128) go(read_kernel<FORMAT, F32, 128>);
