@@ -522,19 +522,36 @@ __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool b
     for (int at = blockIdx.z % sixteens * 16; at < count; at += sixteens * 16) {
         const int64_t t = tokens.list[min(at + lr, count - 1)];
         const float* part = g.part + t * g.N + nb * 16 + lg * 4;
-        f32x4 acc[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = *(const f32x4*)(part + i * 16);
-        for (int s = 1; s < g.splits; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] += *(const f32x4*)(part + (int64_t)s * g.T * g.N + i * 16);
         const char* u = g.U + t * kParts * g.Rp * kEsz + lg * 16;
-        for (int s = 0; s < rs; ++s) {
-            u32x4 uf[kParts], wf[4];
+        u32x4 uf[kParts], wf[4];
+        auto fetch = [&](int s) {
 #pragma unroll
             for (int p = 0; p < kParts; ++p) uf[p] = *(const u32x4*)(u + p * g.Rp * kEsz + s * 64);
 #pragma unroll
             for (int i = 0; i < 4; ++i) wf[i] = *(const u32x4*)(b + ((int64_t)i * rs + s) * 1024);
+        };
+        if (rs) fetch(0);
+        f32x4 acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        auto add = [&](auto qc, int s) {  // parts s .. s + Q - 1, their loads together
+            constexpr int Q = decltype(qc)::value;
+            f32x4 x[Q][4];
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[q][i] = *(const f32x4*)(part + (int64_t)(s + q) * g.T * g.N + i * 16);
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] += x[q][i];
+        };
+        int s = 0;
+        for (; s + 4 <= g.splits; s += 4) add(std::integral_constant<int, 4>{}, s);
+        if (s + 2 <= g.splits) add(std::integral_constant<int, 2>{}, s), s += 2;
+        if (s < g.splits) add(std::integral_constant<int, 1>{}, s);
+        for (int s = 0; s < rs; ++s) {
+            if (s) fetch(s);
 #pragma unroll
             for (int p = 0; p < kParts; ++p)
 #pragma unroll
