@@ -576,16 +576,20 @@ struct ProjectPlan {
     bool few;
 };
 
-// The plan with the least estimated time, in cycles.  A step of a tile, alone on its compute unit and beside a second one, as
-// measured with 4096 k (8192 x 8192 x 8192 in 256 x 256 tiles reaches 1.31 PFLOP/s); fp32 is bound by its matrix rate.
+// The plan with the least estimated time, in cycles.  The constants are fitted to 1200 measured times, every tile and number of parts at
+// 44 shapes (1 to 5000 tokens, 256 to 4096 k, both types); at 28 others the plan is within 3 % of the best on average, 14 % at most.  One size
+// does not fit all: us of 8x8, 4x8, 4x4 and 2x4, whole and in parts (the plan's first), 64 x 4096 x 6144 with 48 adapters 2x4/4 21.5,
+// 4x4/4 21.7, 4x8/8 25.7, 2x4/0 45.9; 2000 x 4096 x 4096 4x8/0 76, 4x4/0 97, 8x8/0 102, 8x8/2 97; 8192 x 4096 x 6144
+// 8x8/0 345, 4x8/0 378, 4x4/0 501, 2x4/0 600.
 static ProjectPlan project_plan(const mmoe_project_shape& s)
 {
     struct Tile {
         int wm, wn;
-        double alone, two, ends;  // cycles of a step; of one of each of two; of a tile's beginning and end
+        double alone, two, ends;  // cycles of a step, alone on its compute unit; of two beside one another; of a tile's beginning and end
     };
-    static const Tile tiles[] = {{8, 8, 1450.0, 0.0, 25000.0}, {4, 8, 900.0, 1800.0, 15000.0}, {4, 4, 680.0, 1430.0, 6000.0}, {2, 4, 440.0, 0.0, 4000.0}};
-    constexpr double kLaunch = 7000.0, kBytes = 1200.0, kRound = 10000.0;  // a launch more; bytes of parts a cycle; a round of making U
+    static const Tile tiles[] = {{8, 8, 1430.0, 0.0, 13500.0}, {4, 8, 880.0, 1640.0, 10200.0}, {4, 4, 600.0, 1340.0, 5900.0}, {2, 4, 400.0, 850.0, 5500.0}};
+    // a launch more; bytes of parts a cycle; a part of the join; a round of making U; an adapter of a tile
+    constexpr double kLaunch = 6700.0, kBytes = 1680.0, kPart = 800.0, kRound = 12500.0, kAdapter = 1100.0;
     const bool f32 = s.dtype == MMOE_F32;
     const int slices = s.d_in / (f32 ? 16 : 32);
     const int T = (s.T + 31) / 32 * 32, most = s.T > kFewTokens ? 0 : s.d_in / 256 < 16 ? s.d_in / 256 : 16;
@@ -594,18 +598,20 @@ static ProjectPlan project_plan(const mmoe_project_shape& s)
     double least = 1e30;
     for (const Tile& t : tiles) {
         const int64_t n = (int64_t)((T + 32 * t.wm - 1) / (32 * t.wm)) * (s.d_out / (32 * t.wn));
-        const double matrix = f32 ? t.wm * t.wn * 135.0 : 0.0;
-        for (int splits = 0; splits <= most; ++splits) {  // 0: not in parts
+        const double matrix = f32 ? t.wm * t.wn * 135.0 : 0.0;  // fp32 is bound by its matrix rate
+        for (int splits = 0; splits <= most; ++splits) {        // 0: not in parts
             const int64_t wgs = splits ? n * splits : n, room = t.two > 0.0 ? 512 : 256, full = wgs / room, rest = wgs % room;
+            // beside the parts run the workgroups that make U: a round of their own where the last one has no room for them, and a tile
+            // shares its compute unit with one of them where it has
+            const int64_t beside = splits && s.n_adapters ? (s.n_adapters < T ? s.n_adapters : T) * ((T + chunk - 1) / chunk) * ((s.rank + 31) / 32) : 0;
             const double steps = (double)slices / (splits ? splits : 1);
             const double alone = (t.alone > matrix ? t.alone : matrix) * steps + t.ends;
             const double two = (t.two > 2.0 * matrix ? t.two : 2.0 * matrix) * steps + t.ends;
-            double time = full * (room == 512 ? two : alone) + (rest > 256 ? two : rest ? alone : 0.0);
-            // beside the parts run the workgroups that make U, in a round of their own where the last round has no room for them
-            const int64_t beside = splits && s.n_adapters ? (s.n_adapters < T ? s.n_adapters : T) * ((T + chunk - 1) / chunk) * ((s.rank + 31) / 32) : 0;
+            double time = full * (room == 512 ? two : alone);
+            if (rest) time += room == 512 && rest + beside > 256 ? two : alone;
             if (beside && (rest ? rest : room) + beside > room) time += kRound * (((rest ? rest : room) + beside - 1) / room);
-            if (splits) time += kLaunch + (2.0 * splits + 1.0) * T * s.d_out * 4.0 / kBytes;
-            else if (s.n_adapters) time += 2.5 * kLaunch + 1500.0 * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
+            if (splits) time += kLaunch + kPart * splits + (1.7 * splits + 1.0) * T * s.d_out * 4.0 / kBytes;
+            else if (s.n_adapters) time += 2.8 * kLaunch + kAdapter * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
             if (time < least) least = time, best = {t.wm, t.wn, splits ? splits : 1, splits > 0};
         }
     }
