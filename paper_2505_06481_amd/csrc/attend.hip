@@ -100,19 +100,23 @@ static Shares shares_of(const mmoe_attend_shape& s)
     r.sets = C <= 32 || three ? 1 : C <= 64 ? 2 : 4;
     const int wide = 16 * r.nc * r.sets;
     r.groups = (int)((C + wide - 1) / wide);
-    // Estimated cycles: a page to a wavefront (its memory share and NC times the work on 16 columns), a request that a workgroup
-    // takes up, and the join (more where a request has many parts).  Wavefronts with different keys take pages at once.
+    // Estimated cycles, fitted to 800 measured times (90 calls of 1 to 100 requests, equal or 2 % to all of the longest, each with up to ten
+    // numbers of shares; the choice is within 4 % of the best on average, 30 % at most): a page to a wavefront, which is its requests' latency
+    // and the work on NC tiles, or its part of the memory's rate where that is more; a request that a workgroup takes up; the join, by parts
+    // and their bytes.  Wavefronts with different keys take pages at once.  us, without shares : with the best number, 32 heads on 8 of
+    // 128: 1 request of 8000 keys bf16 38 : 15; 8 of 1200 to 60000 fp8 448 : 117; 6 of 1500, 40 tokens, fp32 69 : 31; but 32 of 80 to 4000, int8 45 : 56;
+    // 64 of 80 to 4000, bf16 103 : 112.
     const double wide_heads = s.cache.head_dim / 128.0;
-    const double page = s.cache.format != MMOE_CACHE_PLAIN ? 2000.0 + 1500.0 * r.nc * wide_heads
-                        : s.cache.dtype == MMOE_BF16       ? 2500.0 + 1400.0 * r.nc * wide_heads
-                                                           : 3000.0 + 8500.0 * r.nc * wide_heads;
-    constexpr double kRequest = 12000.0, kJoin = 14000.0;
+    const bool codes = s.cache.format != MMOE_CACHE_PLAIN, f32 = s.cache.dtype == MMOE_F32;
+    const double page = (codes ? 2200.0 : f32 ? 2550.0 : 2100.0) * (0.6 + 0.4 * wide_heads) + (codes ? 1260.0 : f32 ? 10500.0 : 740.0) * r.nc * wide_heads;
+    constexpr double kRequest = 7800.0, kJoin = 18800.0, kJoinPart = 73.0, kJoinByte = 1.47e-3, kRate = 3070.0;  // (bytes a cycle)
     const int64_t room = s.cache.head_dim <= 128 && !three ? 512 : 256, heads = (int64_t)s.cache.kv_heads * r.groups;
-    const int kept = s.cache.head_dim * (s.cache.format != MMOE_CACHE_PLAIN ? 1 : (int)elem_size(s.cache.dtype));
-    const double steps = s.cache.format != MMOE_CACHE_PLAIN || kept <= 128 ? 1.0 : kept <= 256 || s.cache.dtype == MMOE_BF16 ? 2.0 : 4.0;  // to a page
-    auto work = [&](double n) { return ceil(n * steps * r.sets / 4.0) * page / steps; };  // n pages
-    const double even = work((double)pages * heads / room);                         // all of it, spread evenly
-    double least = kRequest * ((s.n_requests * heads + room - 1) / room) + (work((double)most_pages) > even ? work((double)most_pages) : even);
+    const int kept = s.cache.head_dim * (codes ? 1 : (int)elem_size(s.cache.dtype));
+    const double bytes = 2.0 * kPage * (kept + (codes ? 4 : 0));                                      // of a page
+    const double steps = codes || kept <= 128 ? 1.0 : kept <= 256 || !f32 ? 2.0 : 4.0;                // to a page
+    auto work = [&](double n, double one) { return ceil(n * steps * r.sets / 4.0) * one / steps; };  // n pages
+    const double even = fmax(work((double)pages * heads / room, page), (double)pages * s.cache.kv_heads * bytes / kRate);  // all of it, spread evenly
+    double least = kRequest * ((s.n_requests * heads + room - 1) / room) + fmax(work((double)most_pages, page), even);
     r.shares = 0;
     if (s.n_requests <= kMaxShared && s.n_requests * (int64_t)s.max_pages < (int64_t)1 << 30) {
         // rounds of resident workgroups, or shares of a few pages
@@ -120,7 +124,10 @@ static Shares shares_of(const mmoe_attend_shape& s)
         for (int64_t w : tries) {
             if (w < 2 || w > kMaxShares || w > pages) continue;
             const double each = (double)pages / w, taken = 1.0 + (double)s.n_requests / w;  // pages, requests of a share
-            const double time = (double)((w * heads + room - 1) / room) * (taken * (work(each / taken) + kRequest)) + kJoin + 200.0 * w / s.n_requests;
+            const double active = fmin((double)w * heads, (double)room) / r.groups;
+            const double one = fmax(page, bytes * active * 4.0 / r.sets / kRate);
+            const double parts = fmin(2.0 * w, (double)(w + s.n_requests)) * heads * fmin((double)C, (double)wide) * s.cache.head_dim * 4.0;
+            const double time = (double)((w * heads + room - 1) / room) * (taken * (work(each / taken, one) + kRequest)) + kJoin + kJoinPart * w / s.n_requests + kJoinByte * parts;
             if (time < least) least = time, r.shares = (int)w;
         }
     }
