@@ -5,8 +5,11 @@
 namespace mmoe {
 
 constexpr int kMaxShares = 4096;
-constexpr int kManyParts = 8;  // of a request on average: four wavefronts join them
+constexpr int kManyParts = 8;  // of a request on average: four wavefronts join them (us, 32 heads, attention with the join by one wavefront and by four:
+                              // 1 request of 60000 keys 37, 31; 4 of 8000 28.2, 26.8; but 8 tokens of 32 requests 67, 76; 512 of 3 242, 299)
 
+// out = sum 2^(m_w - m) O_w / sum 2^(m_w - m) l_w over the shares w that have keys of the row, in their order.  Parts were written just
+// before: 32 requests of 12 tokens, 19 MB of parts, 9.4 us, 2.0 TB/s.
 // Joins the parts of a request that several shares have: WPR wavefronts take a (token, head), each every WPR-th part.
 template <int D, bool F32, int WPR>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)

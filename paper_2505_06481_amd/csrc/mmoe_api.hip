@@ -135,7 +135,7 @@ const char* mmoe_strerror(int status)
         case MMOE_ERR_W3: return "W3 must be given for SWIGLU and must be NULL for RELU and GELU";
         case MMOE_ERR_WORKSPACE: return "workspace missing or smaller than mmoe_workspace_bytes()";
         case MMOE_ERR_ALIGN: return "a pointer is not sufficiently aligned (16 bytes; workspace 256)";
-        case MMOE_ERR_MULTIPLE: return "d_model and d_ff must be multiples of 256";
+        case MMOE_ERR_MULTIPLE: return "d_model and d_ff (d_in and d_out of a projection) must be multiples of 256";
         case MMOE_ERR_LIMIT: return "E, S or the problem size exceeds the library's limits";
         case MMOE_ERR_LAUNCH: return "the HIP runtime refused a kernel launch";
         case MMOE_ERR_STATIC_LIMIT:

@@ -1,5 +1,11 @@
 // Projection shared by the variants with each token's low-rank adapter beside it:
 //   Y[t] = X[t] W + scale[a] (X[t] A[a]) B[a],  a = aid[t].
+//
+// The adapters' two products are thin: they ride on the large one.  U = scale X A is made by a kernel of its own (or beside the large
+// product, where that is cut into parts), and U B is added to the accumulators of X W.  Prefill is bound by the matrix cores
+// (8192 x 4096 x 6144 bf16, 2 adapters of rank 32: 345 us, 1.2 PFLOP/s; 321 without adapters, a library product alone 302 to 320), fp32 by
+// its matrix rate (4096 cubed 918 us, 150 TFLOP/s), few tokens by the weights they read (64 x 4096 x 6144, 48 adapters:
+// 21 us, 3.2 TB/s over both launches) and by the launches (3 tokens: 4.8 + 4.0 us).
 #include "attn_internal.h"
 
 namespace mmoe {
@@ -45,6 +51,8 @@ int launch_pack_pieces(const void* in, void* out, int S, int K, int N, int Kp, i
 // on the bf16 instruction with 16 bits of U, so the adapter adds no error of its own to the rounding of Y.
 //
 // A workgroup takes the tokens of one adapter among a chunk of the batch, 32 at a time; its four wavefronts a quarter of K each.
+// (32 tokens fill two columns' tiles: fewer read the adapter more often, more leave compute units idle.  8192 tokens of 4096, 2 adapters: 26 us,
+// 2.6 TB/s: four rounds of loads, each a memory latency.)
 // A token is read once and an adapter once for each chunk that has tokens of it.  Adapters are numbered by `group`: their own
 // number, or, where they are more than the tokens of a chunk, that of the chunk's first token that uses it.
 struct ShrinkArgs {
@@ -209,7 +217,7 @@ struct ProjectArgs {
     float* part;         // not null: [splits][T][N] parts of X W, which another kernel adds up and the adapters to them
     const int32_t* aid;
     int64_t ldx, ldy;
-    int T, K, N, Rp, n;
+    int T, K, N, R, Rp, n;
     int tiles_m, tiles_n, splits;
 };
 
@@ -224,7 +232,7 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 //   passes the barrier: then step t + 1 is whole, and nobody reads the stage of step t any more;
 //   multiplies step t, reads step t + 1's fragments, and copies step t + kStages into the stage of t.
 // The copies are in assembly and nothing else in the loop is a vector memory instruction, so the waits that
-// order them can count: kStages - 2 steps' copies may be in flight at a barrier.
+// order them can count: kStages - 2 steps' copies may be in flight at a barrier.  What a step takes: at project_plan.
 template <int WM, int WN>
 struct TileLds {
     static constexpr int kStep = (WM + WN) * 2048;  // bytes of a step: 2 WM token fragments, then 2 WN of weights
@@ -506,7 +514,8 @@ __global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_
 }
 
 // Few tokens: Y = the parts of X W, in their order, + U B.  A workgroup takes tokens of one adapter (or of none) among kScan, 16 of
-// every `sixteens` times 16, and 256 features, 64 to a wavefront.
+// every `sixteens` times 16, and 256 features, 64 to a wavefront.  Bound by the latency of a chain (tokens, their list, parts), so parts
+// are loaded four at a time, and few tokens by the B of their adapters (64 tokens of 6144, 48 adapters of rank 16, four parts: 7.6 us).
 template <bool F32>
 __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool by_token, int sixteens)
 {
@@ -527,8 +536,9 @@ __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool b
         auto fetch = [&](int s) {
 #pragma unroll
             for (int p = 0; p < kParts; ++p) uf[p] = *(const u32x4*)(u + p * g.Rp * kEsz + s * 64);
+            const bool ranks = (s * 4 + lg) * (16 / kEsz) < g.R;  // the padding's are zeros, and not read
 #pragma unroll
-            for (int i = 0; i < 4; ++i) wf[i] = *(const u32x4*)(b + ((int64_t)i * rs + s) * 1024);
+            for (int i = 0; i < 4; ++i) wf[i] = ranks ? *(const u32x4*)(b + ((int64_t)i * rs + s) * 1024) : u32x4{0, 0, 0, 0};
         };
         if (rs) fetch(0);
         f32x4 acc[4];
@@ -568,8 +578,10 @@ __global__ __launch_bounds__(256) void project_join_kernel(ProjectArgs g, bool b
 }
 
 // Few tokens run in two launches: parts of X W beside U, then their join with U B.  More in two as well: U, then tiles
-// that add U B themselves.
+// that add U B themselves.  (Parts still pay at 2800 tokens: 2813 x 4096 x 4864, 16 adapters of 64 140 us in one part, 154 whole; their
+// workspace ends at kFewTokens.)
 constexpr int kFewTokens = 4096;
+// One workgroup for all tokens of an adapter in a look is no choice: 512 x 4096 x 512, one adapter, 25 -> 162 us; 4096 x 4096 x 256 39 -> 194.
 static int shrink_chunk(int n, int most) { return 32 * n < most ? 32 * n : most; }
 struct ProjectPlan {
     int wm, wn, splits;
@@ -651,7 +663,7 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
     const int n = s.n_adapters, rp = n ? padded_rank(s) : 0;
     const ProjectPlan p = project_plan(s);
     ProjectArgs g = {(const char*)X, (const char*)Wp, (const char*)Bp, (const char*)ws, (char*)Y, p.few ? (float*)((char*)ws + u_bytes(s)) : nullptr, aid,
-                     ldx, ldy, s.T, s.d_in, s.d_out, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
+                     ldx, ldy, s.T, s.d_in, s.d_out, s.rank, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
     ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, n, (s.rank + 31) / 32, false};
     const int tiles = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
     const dim3 block(256);
@@ -674,7 +686,7 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
         return;
     }
     if (n) {
-        // about 512 workgroups: chunks of 32 tokens and more
+        // about 512 workgroups: chunks of 32 tokens and more.  (One chunk: 8192 x 4096 x 6144, 2 adapters 330 -> 1717 us, 32 adapters 401 -> 512.)
         const int chunks = n >= 512 ? 1 : 512 / n;
         u.chunk = (s.T + chunks - 1) / chunks;
         if (u.chunk < 32) u.chunk = 32;

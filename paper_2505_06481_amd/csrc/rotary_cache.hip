@@ -1,14 +1,16 @@
 // Rotary positions, and the paged cache of keys and values: append (with rotation of the keys) and read back.
 //
-// All three are bound by HBM (a few launches' latency for the tokens of one decode step): every element is read and
-// written once, in 16-byte accesses where its neighbours are in the same thread.
+// All three are bound by HBM (by a launch and a memory latency or two for the tokens of one decode step): every element is read and
+// written once, in 16-byte accesses where its neighbours are in the same thread.  Measured: rotary 8192 tokens of 40 bf16 heads of 128, 30 us,
+// 5.6 TB/s; append 4096 tokens of 8 heads of 128 from bf16 to fp8, 10 us, 2.5 TB/s, and 16384 of them read back, 23 us, 4.4 TB/s; a decode
+// step (16 tokens, 8 heads, int8, keys rotated) 4.9 us, 16 tokens read back 4.6 us; 5 tokens rotated 3.5 us.
 #include <math.h>
 
 #include "attn_internal.h"
 
 namespace mmoe {
 
-// 16 consecutive elements as fp32.
+// Eight consecutive elements as fp32.
 template <bool F32>
 __device__ __forceinline__ void load8(const char* p, float* x)
 {
@@ -45,6 +47,7 @@ __device__ __forceinline__ UnitPlace unit_place(int u, int rot)
     return {16 * u, 16 * u + 8};
 }
 
+// (The angle's error is 2^-25 turn, the rounding to fp32, at any position: a product in fp32 would be off by whole turns from 2^24 on.)
 // Cosine and sine of pairs 8u .. 8u+7 at a position, times m.  steps: turns per position in units of 2^-64; the product's
 // overflow is whole turns.  The upper 32 bits, as a signed number, are the angle in [-1/2, 1/2) turn.
 __device__ __forceinline__ void turn_of(const uint64_t* __restrict__ steps, int pos, float m, float sign, float* c, float* s)
@@ -170,7 +173,8 @@ struct AppendArgs {
     float m, sign;
 };
 
-// A workgroup appends 16 tokens of one head: thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8
+// A head's 8-bit scale is amax / 127 (448), found by its threads through LDS; a value in fp32 times top / amax is rounded once, to the code.
+// A workgroup appends 16 tokens of one head (a value piece holds 16 tokens: fewer would write it twice, more leave compute units idle): thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8
 // each in one piece; values, whose pieces hold several tokens, through LDS, where four tokens in consecutive places become one store.
 // ROTATE: 0 no, 1 halves, 2 neighbours.
 template <int FORMAT, bool F32, int ROTATE, int D>
