@@ -65,6 +65,7 @@ struct ShrinkArgs {
     int chunk;        // tokens
     int groups;       // of a chunk
     int pairs;        // of blocks of 16 ranks: a workgroup takes one
+    int turns;        // workgroups that take 32 tokens of an adapter and chunk in turn
     bool by_token;    // groups are tokens (chunks of up to kScan)
 };
 constexpr int kScan = 512;  // tokens looked through at once
@@ -187,7 +188,7 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
 }
 
 template <bool F32>
-__device__ __forceinline__ void shrink_body(const ShrinkArgs& g, ShrinkLds& lds, int group, int chunk, int rb)
+__device__ __forceinline__ void shrink_body(const ShrinkArgs& g, ShrinkLds& lds, int group, int chunk, int rb, int turn)
 {
     const int t0 = chunk * g.chunk, t1 = min(t0 + g.chunk, g.T);
     const int a = adapter_of(g.aid, t0, t1 - t0, group, g.by_token, g.n);
@@ -197,7 +198,7 @@ __device__ __forceinline__ void shrink_body(const ShrinkArgs& g, ShrinkLds& lds,
     for (int t = t0; t < t1; t += kScan) {
         __syncthreads();  // the list before has been used
         const int count = tokens_of(g.aid, t, min(kScan, t1 - t), a, g.n, lds.tokens);
-        for (int at = 0; at < count; at += 32)
+        for (int at = turn * 32; at < count; at += g.turns * 32)
             if (rb + 1 < real) shrink_tiles<F32, 2>(g, lds, a, rb, cols, at, min(32, count - at));
             else shrink_tiles<F32, 1>(g, lds, a, rb, cols, at, min(32, count - at));
     }
@@ -207,7 +208,7 @@ template <bool F32>
 __global__ __launch_bounds__(256) void shrink_kernel(ShrinkArgs g)
 {
     __shared__ ShrinkLds lds;
-    shrink_body<F32>(g, lds, blockIdx.y, blockIdx.x, blockIdx.z * 2);
+    shrink_body<F32>(g, lds, blockIdx.y, blockIdx.x, blockIdx.z % g.pairs * 2, blockIdx.z / g.pairs);
 }
 
 // ---- Y = X W + U B -----------------------------------------------------------------------------------
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_
     if ((int)blockIdx.x < tiles) tile_body<F32, WM, WN>(g, lds.tile, blockIdx.x, tiles);
     else {
         const int id = blockIdx.x - tiles, pair = id % u.pairs, of = id / u.pairs;
-        shrink_body<F32>(u, lds.shrink, of % u.groups, of / u.groups, pair * 2);
+        shrink_body<F32>(u, lds.shrink, of % u.groups, of / u.groups, pair * 2, 0);
     }
 }
 
@@ -664,7 +665,7 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
     const ProjectPlan p = project_plan(s);
     ProjectArgs g = {(const char*)X, (const char*)Wp, (const char*)Bp, (const char*)ws, (char*)Y, p.few ? (float*)((char*)ws + u_bytes(s)) : nullptr, aid,
                      ldx, ldy, s.T, s.d_in, s.d_out, s.rank, rp, n, (s.T + 32 * p.wm - 1) / (32 * p.wm), s.d_out / (32 * p.wn), p.splits};
-    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, n, (s.rank + 31) / 32, false};
+    ShrinkArgs u = {(const char*)X, (const char*)Ap, aid, scale, (char*)ws, ldx, s.T, s.d_in, s.rank, rp, n, s.T, n, (s.rank + 31) / 32, 1, false};
     const int tiles = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
     const dim3 block(256);
     if (p.few) {
@@ -690,7 +691,11 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
         const int chunks = n >= 512 ? 1 : 512 / n;
         u.chunk = (s.T + chunks - 1) / chunks;
         if (u.chunk < 32) u.chunk = 32;
-        hipLaunchKernelGGL(shrink_kernel<F32>, dim3((s.T + u.chunk - 1) / u.chunk, n, u.pairs), block, 0, st, u);
+        // An adapter's tokens may follow one another and be most of a chunk: up to four workgroups to them.  (8192 x 4096 x 1024, us with one and
+        // four: 32 adapters in blocks 152, 100, in turns of chance 105, 105; 8 in blocks 112, 92.  Over two looks the looking costs more: 20000
+        // tokens, 500 adapters 66, 129.)
+        u.turns = u.chunk > 2 * kScan ? 1 : u.chunk < 128 ? u.chunk / 32 : 4;
+        hipLaunchKernelGGL(shrink_kernel<F32>, dim3((s.T + u.chunk - 1) / u.chunk, n, u.pairs * u.turns), block, 0, st, u);
     }
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles), block, 0, st, g); };
     if (p.wm == 8) go(project_tile_kernel<F32, 8, 8>);

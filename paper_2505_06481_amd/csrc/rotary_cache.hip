@@ -173,7 +173,7 @@ struct AppendArgs {
     float m, sign;
 };
 
-// A head's 8-bit scale is amax / 127 (448), found by its threads through LDS; a value in fp32 times top / amax is rounded once, to the code.
+// A head's 8-bit scale is amax / 127 (448), found between its lanes; a value in fp32 times top / amax is rounded once, to the code.
 // A workgroup appends 16 tokens of one head (a value piece holds 16 tokens: fewer would write it twice, more leave compute units idle): thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8
 // each in one piece; values, whose pieces hold several tokens, through LDS, where four tokens in consecutive places become one store.
 // ROTATE: 0 no, 1 halves, 2 neighbours.
@@ -185,7 +185,6 @@ __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs g)
     constexpr int U = D / 16, kThreads = 2 * kTok * U;
     const int tid = threadIdx.x;
     __shared__ __attribute__((aligned(16))) char codes[kTok * D * P::kBytes];  // [kTok][D] of V
-    __shared__ float amax[P::kPlain ? 1 : 2 * kTok * U];                        // [2][kTok][U]
     __shared__ int place[kTok];
     const int t0 = blockIdx.x * kTok, h = blockIdx.y;
     const int which = tid / (kTok * U), tok = tid / U % kTok, u = tid % U;  // which: 0 keys, 1 values
@@ -217,10 +216,12 @@ __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs g)
             a = fmaxf(a, fabsf(x[i]));
             odd = odd || !(fabsf(x[i]) < INFINITY);
         }
-        amax[(which * kTok + tok) * U + u] = odd ? INFINITY : a;
-        __syncthreads();
-        a = 0.0f;
-        for (int i = 0; i < U; ++i) a = fmaxf(a, amax[(which * kTok + tok) * U + i]);
+        // over the head's U lanes
+        if (odd) a = INFINITY;
+        a = fmaxf(a, lane_xor<1>(a));
+        a = fmaxf(a, lane_xor<2>(a));
+        if constexpr (U >= 8) a = fmaxf(a, lane_xor<4>(a));
+        if constexpr (U >= 16) a = fmaxf(a, lane_xor<8>(a));
         const bool fine = a < INFINITY && a >= kLeast;
         const float inv = fine ? kTop[FORMAT] / a : 0.0f;
         const float scale = a < INFINITY ? (fine ? a * (float)(1.0 / (double)kTop[FORMAT]) : 0.0f) : NAN;
