@@ -84,9 +84,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
     if (lane == 0 && g.lse) g.lse[t * g.heads + head] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * 0.693147180559945309417f;
 }
 
-static Shares shares_of(const mmoe_attend_shape& s)
+// The shares with the least estimated time for `sets` sets of columns at most.
+static double shares_for(const mmoe_attend_shape& s, int sets, Shares& r)
 {
-    Shares r;
     const int G = s.heads / s.cache.kv_heads;
     const int64_t C = (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * G;
     const int64_t cap = (int64_t)s.max_pages * kPage;
@@ -100,7 +100,7 @@ static Shares shares_of(const mmoe_attend_shape& s)
     // bf16 (30000) 196 : 188, fp32 (15000) 311 : 252, heads of 64, fp8 137 : 129.  (64 columns so: fp8 233 : 224, bf16 205 : 228.)
     const bool three = C > 32 && C <= 48 && s.cache.head_dim <= 128 && pages * s.cache.kv_heads >= 100 * 256;
     r.nc = C <= 16 ? 1 : three ? 3 : 2;
-    r.sets = C <= 32 || three ? 1 : C <= 64 ? 2 : 4;
+    r.sets = C <= 32 || three ? 1 : C <= 64 ? 2 : sets;
     const int wide = 16 * r.nc * r.sets;
     r.groups = (int)((C + wide - 1) / wide);
     // Estimated cycles, fitted to 800 measured times (90 calls of 1 to 100 requests, equal or 2 % to all of the longest, each with up to ten
@@ -134,7 +134,15 @@ static Shares shares_of(const mmoe_attend_shape& s)
             if (time < least) least = time, r.shares = (int)w;
         }
     }
-    return r;
+    return least;
+}
+
+// More than 64 columns: four sets read a page once for 128, two sets and more groups spread few requests over more compute units.  us, four : two: 2
+// requests of 100 tokens over 500 keys, heads of 256 51 : 34; 28 of 50 over 400, fp32 64 : 53; 8 of 128 over 1000, int8 47 : 42; but 64 of 32 over 500 40 : 48.
+static Shares shares_of(const mmoe_attend_shape& s)
+{
+    Shares two, four;
+    return shares_for(s, 2, two) < shares_for(s, 4, four) ? two : four;
 }
 
 // Whether the grids' sizes fit.

@@ -601,10 +601,11 @@ static ProjectPlan project_plan(const mmoe_project_shape& s)
         double alone, two, ends;  // cycles of a step, alone on its compute unit; of two beside one another; of a tile's beginning and end
     };
     static const Tile tiles[] = {{8, 8, 1430.0, 0.0, 13500.0}, {4, 8, 880.0, 1640.0, 10200.0}, {4, 4, 600.0, 1340.0, 5900.0}, {2, 4, 400.0, 850.0, 5500.0}};
-    // a launch more; bytes of parts a cycle; a part of the join; a round of making U; an adapter of a tile
-    constexpr double kLaunch = 6700.0, kBytes = 1680.0, kPart = 800.0, kRound = 12500.0, kAdapter = 1100.0;
+    // a launch more; bytes of parts a cycle; a part of the join; a round of making U; an adapter of a tile, and
+    // 64 bytes of its rank (12 adapters of 128, 2034 x 1792 x 4608: 129 us whole, 93 with the adapters in the join; of 16 71 either way)
+    constexpr double kLaunch = 6700.0, kBytes = 1680.0, kPart = 800.0, kRound = 12500.0, kAdapter = 300.0, kRanks = 2500.0;
     const bool f32 = s.dtype == MMOE_F32;
-    const int slices = s.d_in / (f32 ? 16 : 32);
+    const int slices = s.d_in / (f32 ? 16 : 32), ranks = s.n_adapters ? padded_rank(s) / (f32 ? 16 : 32) : 0;
     const int T = (s.T + 31) / 32 * 32, most = s.T > kFewTokens ? 0 : s.d_in / 256 < 16 ? s.d_in / 256 : 16;
     const int chunk = s.n_adapters ? shrink_chunk(s.n_adapters, kScan) : kScan;
     ProjectPlan best = {8, 8, 1, false};
@@ -624,7 +625,7 @@ static ProjectPlan project_plan(const mmoe_project_shape& s)
             if (rest) time += room == 512 && rest + beside > 256 ? two : alone;
             if (beside && (rest ? rest : room) + beside > room) time += kRound * (((rest ? rest : room) + beside - 1) / room);
             if (splits) time += kLaunch + kPart * splits + (1.7 * splits + 1.0) * T * s.d_out * 4.0 / kBytes;
-            else if (s.n_adapters) time += 2.8 * kLaunch + kAdapter * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
+            else if (s.n_adapters) time += 2.0 * kLaunch + (kAdapter + kRanks * ranks) * (s.n_adapters < 32 * t.wm ? s.n_adapters : 32 * t.wm);
             if (time < least) least = time, best = {t.wm, t.wn, splits ? splits : 1, splits > 0};
         }
     }
