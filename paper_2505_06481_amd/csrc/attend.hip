@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs g)
 }
 
 // The shares with the least estimated time for `sets` sets of columns at most.
-static double shares_for(const mmoe_attend_shape& s, int sets, Shares& r)
+static double shares_for(const mmoe_attend_shape& s, int sets, bool three, Shares& r)  // three: tiles to a wavefront
 {
     const int G = s.heads / s.cache.kv_heads;
     const int64_t C = (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * G;
@@ -93,12 +93,6 @@ static double shares_for(const mmoe_attend_shape& s, int sets, Shares& r)
     const int64_t longest = s.max_keys && s.max_keys < cap ? s.max_keys : cap;
     const int64_t sum = s.sum_keys ? s.sum_keys : (int64_t)s.n_requests * longest;
     const int64_t pages = sum / kPage + s.n_requests, most_pages = (longest + kPage - 1) / kPage;
-    // 32 columns to a wavefront leave room for a second one on its SIMD, whose vector instructions run under the first one's matrix
-    // instructions.  33 to 48 columns are two sets of them, or, with long contexts, three tiles to a lone wavefront, which reads the keys
-    // once.  Two sets : three tiles, us: 11 requests of 10 tokens over 2900 keys, int8, 40 columns 27.7 : 32.0; 32 over 6000 71.9 : 80.0 (46
-    // pages to a compute unit); 7 over 11000 38.8 : 46.2; but 8 over 60000, 48 columns (234 pages) fp8 246 : 199, int8 257 : 201,
-    // bf16 (30000) 196 : 188, fp32 (15000) 311 : 252, heads of 64, fp8 137 : 129.  (64 columns so: fp8 233 : 224, bf16 205 : 228.)
-    const bool three = C > 32 && C <= 48 && s.cache.head_dim <= 128 && pages * s.cache.kv_heads >= 100 * 256;
     r.nc = C <= 16 ? 1 : three ? 3 : 2;
     r.sets = C <= 32 || three ? 1 : C <= 64 ? 2 : sets;
     const int wide = 16 * r.nc * r.sets;
@@ -111,8 +105,10 @@ static double shares_for(const mmoe_attend_shape& s, int sets, Shares& r)
     // 64 of 80 to 4000, bf16 103 : 112.
     const double wide_heads = s.cache.head_dim / 128.0;
     const bool codes = s.cache.format != MMOE_CACHE_PLAIN, f32 = s.cache.dtype == MMOE_F32;
-    const double page = (codes ? 2200.0 : f32 ? 2550.0 : 2100.0) * (0.6 + 0.4 * wide_heads) + (codes ? 1260.0 : f32 ? 10500.0 : 740.0) * r.nc * wide_heads;
-    constexpr double kRequest = 7800.0, kJoin = 18800.0, kJoinPart = 73.0, kJoinByte = 1.47e-3, kRate = 3070.0;  // (bytes a cycle)
+    const double alone = !three ? 1.0 : codes ? 0.8 : f32 ? 0.7 : 0.9;  // a lone wavefront's page
+    const double page = alone * ((codes ? 2200.0 : f32 ? 2550.0 : 2100.0) * (0.6 + 0.4 * wide_heads) + (codes ? 1260.0 : f32 ? 10500.0 : 740.0) * r.nc * wide_heads);
+    const double kRequest = three ? 15600.0 : 7800.0;
+    constexpr double kJoin = 18800.0, kJoinPart = 73.0, kJoinByte = 1.47e-3, kRate = 3070.0;  // (bytes a cycle)
     const int64_t room = s.cache.head_dim <= 128 && !three ? 512 : 256, heads = (int64_t)s.cache.kv_heads * r.groups;
     const int kept = s.cache.head_dim * (codes ? 1 : (int)elem_size(s.cache.dtype));
     const double bytes = 2.0 * kPage * (kept + (codes ? 4 : 0));                                      // of a page
@@ -137,12 +133,24 @@ static double shares_for(const mmoe_attend_shape& s, int sets, Shares& r)
     return least;
 }
 
+// 32 columns to a wavefront leave room for a second one on its SIMD, whose vector instructions run under the first one's matrix instructions.
+// 33 to 48 columns are two sets of them, or three tiles to a lone wavefront, which reads and converts the keys once.  us, two sets : three
+// tiles, 32 heads on 8 of 128: 32 requests of 12 tokens over 3000 keys int8 62 : 49, 8 over 60000 fp8 225 : 200, 28 over 1000 fp32 100 : 76; but
+// 64 over 700 fp8 31 : 45, 11 of 10 over 2900 int8 40 : 46, 32 over 3000 bf16 79 : 81.  (64 columns so: 60000, fp8 233 : 224, bf16 205 : 228.)
 // More than 64 columns: four sets read a page once for 128, two sets and more groups spread few requests over more compute units.  us, four : two: 2
 // requests of 100 tokens over 500 keys, heads of 256 51 : 34; 28 of 50 over 400, fp32 64 : 53; 8 of 128 over 1000, int8 47 : 42; but 64 of 32 over 500 40 : 48.
 static Shares shares_of(const mmoe_attend_shape& s)
 {
-    Shares two, four;
-    return shares_for(s, 2, two) < shares_for(s, 4, four) ? two : four;
+    Shares r, other;
+    double least = shares_for(s, 2, false, r);
+    auto also = [&](int sets, bool three) {
+        const double time = shares_for(s, sets, three, other);
+        if (time < least) least = time, r = other;
+    };
+    also(4, false);
+    const int64_t C = (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * (s.heads / s.cache.kv_heads);
+    if (C > 32 && C <= 48 && s.cache.head_dim <= 128) also(1, true);
+    return r;
 }
 
 // Whether the grids' sizes fit.
