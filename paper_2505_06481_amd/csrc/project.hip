@@ -509,8 +509,8 @@ __global__ __launch_bounds__(256, WM * WN > 32 || WM == 2 ? 1 : 2) void project_
     } lds;
     if ((int)blockIdx.x < tiles) tile_body<F32, WM, WN>(g, lds.tile, blockIdx.x, tiles);
     else {
-        const int id = blockIdx.x - tiles, pair = id % u.pairs, of = id / u.pairs;
-        shrink_body<F32>(u, lds.shrink, of % u.groups, of / u.groups, pair * 2, 0);
+        const int id = blockIdx.x - tiles, pair = id % u.pairs, turn = id / u.pairs % u.turns, of = id / (u.pairs * u.turns);
+        shrink_body<F32>(u, lds.shrink, of % u.groups, of / u.groups, pair * 2, turn);
     }
 }
 
@@ -676,14 +676,19 @@ static void project(const mmoe_project_shape& s, const void* X, const int32_t* a
         // U: about 32 tokens of an adapter to a workgroup, so that it is done before the tiles are
         u.chunk = by_token ? chunk : shrink_chunk(n, chunk);
         u.groups = by_token ? chunk : n;
-        const dim3 grid(tiles + (n ? u.groups * u.pairs * ((s.T + u.chunk - 1) / u.chunk) : 0));
+        // (two, where few adapters leave them room beside the tiles: us with one and two, 200 x 2048 x 2048, 3 adapters 20.6, 18.7, in blocks
+        // 24.7, 19.5; 400, 8 20.1, 19.4; but 2000 x 4096 x 1024, 16 adapters 41, 47, in blocks 64, 61)
+        if (!by_token && u.chunk >= 64 && n <= 8) u.turns = 2;
+        const dim3 grid(tiles + (n ? u.groups * u.pairs * u.turns * ((s.T + u.chunk - 1) / u.chunk) : 0));
         auto parts = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g, u, tiles); };
         if (p.wm == 8) parts(project_parts_kernel<F32, 8, 8>);
         else if (p.wn == 8) parts(project_parts_kernel<F32, 4, 8>);
         else if (p.wm == 4) parts(project_parts_kernel<F32, 4, 4>);
         else parts(project_parts_kernel<F32, 2, 4>);
-        // as many workgroups to an adapter as its even share of the tokens has sixteens
-        const int groups = by_token ? chunk : n + 1, sixteens = (chunk + 16 * groups - 1) / (16 * groups);
+        // twice as many workgroups to an adapter as its even share of the tokens has sixteens (200 x 2048 x 2048 18.7 -> 17.2; 4000 x 1024 x 1024, 32
+        // adapters in blocks 52.4 -> 48.7)
+        const int groups = by_token ? chunk : n + 1, most = (chunk + 15) / 16,
+                  even = (chunk + 16 * groups - 1) / (16 * groups), sixteens = 2 * even < most ? 2 * even : most;
         hipLaunchKernelGGL(project_join_kernel<F32>, dim3(s.d_out / 256, groups, chunks * sixteens), block, 0, st, g, by_token, sixteens);
         return;
     }

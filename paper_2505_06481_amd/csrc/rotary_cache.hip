@@ -174,8 +174,9 @@ struct AppendArgs {
 };
 
 // A head's 8-bit scale is amax / 127 (448), found between its lanes; a value in fp32 times top / amax is rounded once, to the code.
-// A workgroup appends 16 tokens of one head (a value piece holds 16 tokens: fewer would write it twice, more leave compute units idle): thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8
-// each in one piece; values, whose pieces hold several tokens, through LDS, where four tokens in consecutive places become one store.
+// A workgroup appends 16 tokens of one head (a value piece holds 16 tokens: fewer would write it twice, more leave compute units
+// idle): thread (matrix, token, unit) has 16 elements.  Keys go out from there, two runs of 8 each in one piece; values, whose pieces
+// hold several tokens, through LDS, where four tokens in consecutive places become one store.
 // ROTATE: 0 no, 1 halves, 2 neighbours.
 template <int FORMAT, bool F32, int ROTATE, int D>
 __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs g)
