@@ -192,6 +192,13 @@ def test_project_chunks_of_tokens(at, ref, T, n, R, dtype):
     run_project(at, ref, T, 256, 256, n, R, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,n,R", [(200, 3, 16), (511, 8, 40), (900, 9, 16), (4100, 2, 33), (5000, 32, 16), (4500, 140, 8)])
+def test_project_runs_of_tokens(at, ref, T, n, R, dtype):
+    """Each adapter's tokens one after the other: several workgroups share them."""
+    run_project(at, ref, T, 256, 512, n, R, dtype, mix="blocks")
+
+
 @pytest.mark.parametrize("T,K,N,n,dtype", [(2048, 2048, 2048, 4, "bf16"), (4096, 1024, 1024, 3, "bf16"), (8200, 512, 8192, 2, "bf16"), (256, 8192, 512, 4, "bf16"),
                                            (600, 4096, 2048, 3, "f32"), (2000, 2048, 1024, 3, "f32")])
 def test_project_tiles(at, ref, T, K, N, n, dtype):
