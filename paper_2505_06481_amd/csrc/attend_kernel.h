@@ -352,7 +352,9 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         l[decltype(ct)::value] = 0.0f;  // this lane's keys only, until the end
         each<DT>([&](auto dt) { o[decltype(ct)::value][decltype(dt)::value] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
     });
-    int lift = -126;  // o holds 2^(kLiftBits - lift) times its value (codes): lift is the largest exponent of a value scale so far
+    // o holds 2^(kLiftBits - lift) times its value (codes): lift is the largest exponent of a value scale so far.  Scales that are not zero are 2^-109
+    // at least; with zeros only, from where it starts, that factor is 2^125: a finite one.
+    int lift = -118;
 
     // Accumulators are read by vector instructions in rare branches only: they stay in AGPRs around them.
     auto pin = [&](int ct) {
