@@ -2,7 +2,8 @@
 //
 // out[t,h] = sum_j softmax_j(scale <Q[t,h], K[j]>) V[j], in one pass over the keys with a reference m for the exponents and the
 // sum l: O holds sum 2^(s_j - m) V_j, and where a step's largest score exceeds m by more than kSlack, m becomes that score and O and
-// l are scaled (everything in base 2: the scores carry log2 e).
+// l are scaled (everything in base 2: the scores carry log2 e).  Over 8-bit pages m follows the products of probabilities and value scales
+// that the column sees in the same way, by column: what a row that is hidden or all but improbable holds takes no bits from the others.
 //
 // A column is a (token, query head) pair of one request and key head: all that read the same keys.  A wavefront holds 16 NC
 // columns.  Keys are the row operand of the first product, so a lane has four consecutive keys of a column per tile of 16, which
@@ -15,8 +16,8 @@
 // latency (4 requests of up to 700: 9.7 us).  8-bit codes widen to fp16, which holds them exactly; their key scales multiply scores and
 // their value scales probabilities, so pages are never written out in 16 bits.
 //
-// Roundings below 32 bits: probabilities to bf16 or, lifted by a power of two, fp16, the operand type of the second product (8 and
-// 11 bits of numbers that are summed; the sum l has them in fp32); with codes queries to fp16 too, scaled by a power of two (exact but for
+// Roundings below 32 bits: probabilities to bf16 or, with their value's scale, fp16, the operand type of the second product (8 and
+// 11 bits of numbers that are summed, fp16 to 2^-30 of the largest; the sum l has them in fp32); with codes queries to fp16 too, scaled by a power of two (exact but for
 // elements under 2^-26 of the head's largest); out once.
 #pragma once
 #include <math.h>
@@ -123,13 +124,21 @@ __device__ __forceinline__ float sum_groups(float x)
 
 __device__ __forceinline__ void in_agprs(f32x4& x) { asm volatile("" : "+a"(x)); }
 
+// What is worked out of it in a rare branch is not worked out ahead of the branch.
+template <typename T>
+__device__ __forceinline__ void only_here(T& x) { asm volatile("" : "+v"(x)); }
+
 // 2^x; -infinity gives 0.
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Probabilities are up to 2^8: scores that rise slowly then leave O and l as they are.  (Random keys: level, 202 us with, 199 without;
 // the scaling of 64 registers where every step has a new maximum is what it spares.)
 constexpr float kSlack = 8.0f;
-constexpr int kLiftBits = 7;    // fp16 ones are lifted by 2^7 (to 2^15 at most), which keeps small ones out of the subnormal range
+// Over codes the reference follows the products of probabilities and value scales, which go into fp16: a column's largest one is under 2^7 when it is
+// found and may rise to 2^15, which keeps small ones out of the subnormal range.  Rows that the column does not see have no part in it.
+// Scales that are not zero are 2^-109 at least, so l could leave fp32: probabilities are 2^60 to 2^-90 of the reference at their peak, and what that
+// leaves of the lift is kept apart, by column.
+constexpr float kLiftBits = 7.0f, kTopBits = 15.0f, kMostBits = 100.0f;
 
 template <int D, int KIND, int NC>
 struct AttendPlan {
@@ -352,9 +361,9 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
         l[decltype(ct)::value] = 0.0f;  // this lane's keys only, until the end
         each<DT>([&](auto dt) { o[decltype(ct)::value][decltype(dt)::value] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
     });
-    // o holds 2^(kLiftBits - lift) times its value (codes): lift is the largest exponent of a value scale so far.  Scales that are not zero are 2^-109
-    // at least; with zeros only, from where it starts, that factor is 2^125: a finite one.
-    int lift = -118;
+    float apart[NC];  // codes: o holds 2^apart times what the reference says
+    each<NC>([&](auto ct) { apart[decltype(ct)::value] = 0.0f; });
+    bool aparts = false;  // one of them is not zero
 
     // Accumulators are read by vector instructions in rare branches only: they stay in AGPRs around them.
     auto pin = [&](int ct) {
@@ -418,6 +427,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             each<DT>([&](auto dt) { load_v(block, step, dt); });
             __builtin_amdgcn_sched_barrier(0);
         }
+        float room = 0.0f;  // codes: bits by which a probability may exceed the reference, whichever value it goes with
         if constexpr (kCodes) {
             each<KT>([&](auto ktc) {
                 constexpr int kt = decltype(ktc)::value;
@@ -431,18 +441,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             float most = 0.0f;
             each<KT * 4>([&](auto x) { most = fmaxf(most, vs[decltype(x)::value / 4][decltype(x)::value % 4]); });
             most = max_groups(most);
-            // exponent above the largest: scale * 2^-here < 1
-            const int here = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(most) >> 23) - 126);
-            const int above = max(lift, min(here, 127));
-            each<NC>([&](auto ct) { pin(decltype(ct)::value); });
-            if (above != lift) {
-                const float down = ldexpf(1.0f, max(lift - above, -140));
-                each<NC * DT>([&](auto x) { o[decltype(x)::value / DT][decltype(x)::value % DT] *= down; });
-                lift = above;
-                each<NC>([&](auto ct) { pin(decltype(ct)::value); });
-            }
-            const float up = ldexpf(1.0f, kLiftBits - lift);
-            each<KT>([&](auto kt) { vs[decltype(kt)::value] *= up; });
+            room = most > 0.0f ? kTopBits - (float)__builtin_amdgcn_frexp_expf(most) : kMostBits;  // (the scale is under 2^frexp)
         }
         load_k(next_block, ahead);
         if constexpr (!kLate) load_ks(next_block);
@@ -484,7 +483,33 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             each<KT * 4>([&](auto x) { top = fmaxf(top, s[ct][decltype(x)::value / 4][decltype(x)::value % 4]); });
             top = max_groups(top) * mult[ct];
             pin(ct);
-            if (__any(top - m[ct] > kSlack)) {  // (never where top is -infinity)
+            if constexpr (kCodes) {
+                if (__any(top - m[ct] > fminf(room - apart[ct], kMostBits))) {  // (never where top is -infinity)
+                    each<KT>([&](auto kt) { only_here(s[ct][decltype(kt)::value]), only_here(vs[decltype(kt)::value]); });
+                    const bool first = m[ct] == -INFINITY;
+                    const float from = !first ? m[ct] : top == -INFINITY ? 0.0f : top;
+                    float most = -INFINITY;  // log2 of the largest product that the column sees: a scale's bits are 2^23 (log2 + 127) less 0 to 0.09
+                    each<KT * 4>([&](auto x) {
+                        constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
+                        most = fmaxf(most, __builtin_fmaf((float)__float_as_uint(vs[kt][e]), 0x1p-23f, __builtin_fmaf(s[ct][kt][e], mult[ct], -from)));
+                    });
+                    most = max_groups(most) - 126.9f + apart[ct];
+                    const float peak = fmaxf(__log2f(max_groups(l[ct])), top - from);  // bits of the largest probability, or of a part of l
+                    const float by = first || most > kTopBits ? most - kLiftBits : 0.0f;  // too many
+                    float up = fminf(fmaxf(by, peak - 90.0f), peak + 60.0f);
+                    if (!(fabsf(from) < 0x1p20f)) up = fmaxf(top - from, 0.0f);  // so far off that references are no longer so near one another
+                    const bool none = peak == -INFINITY;
+                    m[ct] = none ? -INFINITY : from + up;
+                    up = none ? 0.0f : m[ct] - from;
+                    const float rest = fabsf(up - by) > 1.0f ? fminf(apart[ct] + (up - by), 115.0f - fmaxf(peak - up, 0.0f)) : apart[ct];
+                    const float f = pow2(rest - apart[ct] - up);
+                    each<DT>([&](auto dt) { o[ct][decltype(dt)::value] *= f; });
+                    l[ct] *= pow2(-up);
+                    apart[ct] = rest;
+                    aparts = aparts || __any(rest != 0.0f);
+                    pin(ct);
+                }
+            } else if (__any(top - m[ct] > kSlack)) {  // (never where top is -infinity)
                 const float up = fmaxf(m[ct], top), alpha = pow2(m[ct] - (up == -INFINITY ? 0.0f : up));
                 m[ct] = up;
                 l[ct] *= alpha;
@@ -495,15 +520,21 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             float sum = 0.0f;
             each<KT * 4>([&](auto x) {
                 constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
-                const float y = pow2(__builtin_fmaf(s[ct][kt][e], mult[ct], -base));
-                sum += y;
-                s[ct][kt][e] = kCodes ? y * vs[kt][e] : y;
+                s[ct][kt][e] = pow2(__builtin_fmaf(s[ct][kt][e], mult[ct], -base));
+                sum += s[ct][kt][e];
             });
-            if (kCodes && tail)  // 0 times a scale that is not a number
-                each<KT * 4>([&](auto x) {
-                    constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
-                    if (!(vis[ct] & (uint64_t)1 << (kt * 16 + e))) s[ct][kt][e] = 0.0f;
-                });
+            if constexpr (kCodes) {
+                if (aparts) {
+                    const float f = pow2(apart[ct]);
+                    each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= f; });
+                }
+                each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= vs[decltype(kt)::value]; });
+                if (tail)  // 0 times a scale that is not a number
+                    each<KT * 4>([&](auto x) {
+                        constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
+                        if (!(vis[ct] & (uint64_t)1 << (kt * 16 + e))) s[ct][kt][e] = 0.0f;
+                    });
+            }
             l[ct] += sum;
             // tiles to operand pieces: 16-bit ones hold two tiles' keys
             if constexpr (KIND == kF32) {
@@ -620,15 +651,19 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
 
     // ---- results ----
     tid = fresh(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
-    if constexpr (kCodes) {
-        const float down = ldexpf(1.0f, max(lift - kLiftBits, -140));
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[ct][dt] *= down;
-    }
 #pragma unroll
     for (int ct = 0; ct < NC; ++ct) l[ct] = sum_groups(l[ct]);
+    if constexpr (kCodes) {  // the reference to where l is between 1/2 and 1
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) {
+            const int bits = __builtin_amdgcn_frexp_expf(l[ct]);
+            const float down = ldexpf(pow2(-apart[ct]), -bits);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[ct][dt] *= down;
+            l[ct] = ldexpf(l[ct], -bits);
+            m[ct] += (float)bits;
+        }
+    }
 
     const bool direct = slot < 0;
     const int64_t part = (((int64_t)share * 2 + slot) * g.kv_heads + h) * g.columns;

@@ -1,8 +1,9 @@
 """Attention over 8-bit pages whose value scales are zero or far apart, against the plain 64-bit definitions in oracle/attention.py.
 
 Tolerances.  Codes are exact, a probability times its scale is rounded to fp16 (2^-11 of it), scores are sums of at most 256 terms in fp32
-(2^-11 of a probability for scores of a few hundred), and the output is rounded to bf16 (u = 2^-8): |err| <= 2^-9 sum p |v| + u |out|, with the
-probabilities and values of the row itself.
+(2^-11 of a probability for scores of a few hundred), and the output is rounded to bf16 (u = 2^-8).  Products far below the row's largest are
+subnormal in fp16, to the nearest 2^-24: off by 2^-25 where the largest is 2^5 or more, and times a code, at most 2^-30 of the largest
+product times value for each of n keys.  |err| <= 2^-9 sum p |v| + u |out| + 2^-30 n sum p amax, with the row's own probabilities and values.
 """
 import pytest
 import torch
@@ -27,9 +28,10 @@ def check(at, ref, p, D, tree, scale=None, H=4, **hints):
     torch.cuda.synchronize()
     want, want_lse = ref.attend(p.Q, p.starts, p.ctx, tree, p.keys, p.values, scale)
     size, _ = ref.attend(p.Q, p.starts, p.ctx, tree, p.keys, [v.abs() for v in p.values], scale)
+    floor, _ = ref.attend(p.Q, p.starts, p.ctx, tree, p.keys, [v.abs().amax(-1, keepdim=True).expand(v.shape) for v in p.values], scale)
     what = f"ctx={p.ctx} drafts={p.drafts} D={D} {hints}"
     close(lse, want_lse, 1e-5 * (1 + want_lse.abs().nan_to_num(0, 0, 0)), what + " lse")
-    close(out, want, 2.0 ** -9 * size + 2.0 ** -8 * want.abs(), what)
+    close(out, want, 2.0 ** -9 * size + 2.0 ** -8 * want.abs() + 2.0 ** -30 * max(len(k) for k in p.keys) * floor, what)
     return out
 
 
