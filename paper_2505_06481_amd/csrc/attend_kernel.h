@@ -481,30 +481,32 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             }
             float top = -INFINITY;
             each<KT * 4>([&](auto x) { top = fmaxf(top, s[ct][decltype(x)::value / 4][decltype(x)::value % 4]); });
-            top = max_groups(top) * mult[ct];
+            const float score = max_groups(top);
+            top = score * mult[ct];
             pin(ct);
             if constexpr (kCodes) {
-                if (__any(top - m[ct] > fminf(room - apart[ct], kMostBits))) {  // (never where top is -infinity)
+                // (never where top is -infinity; not top - m: far off, its rounding is many bits that the exponents do not have)
+                if (__any(__builtin_fmaf(score, mult[ct], -m[ct]) > fminf(room - apart[ct], kMostBits))) {
                     each<KT>([&](auto kt) { only_here(s[ct][decltype(kt)::value]), only_here(vs[decltype(kt)::value]); });
-                    const bool first = m[ct] == -INFINITY;
-                    const float from = !first ? m[ct] : top == -INFINITY ? 0.0f : top;
+                    const float high = fmaxf(m[ct], top);
+                    const bool none = high == -INFINITY;
+                    const float from = none ? 0.0f : high, gap = from - m[ct];  // (infinite where there was nothing so far)
                     float most = -INFINITY;  // log2 of the largest product that the column sees: a scale's bits are 2^23 (log2 + 127) less 0 to 0.09
                     each<KT * 4>([&](auto x) {
                         constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
                         most = fmaxf(most, __builtin_fmaf((float)__float_as_uint(vs[kt][e]), 0x1p-23f, __builtin_fmaf(s[ct][kt][e], mult[ct], -from)));
                     });
                     most = max_groups(most) - 126.9f + apart[ct];
-                    const float peak = fmaxf(__log2f(max_groups(l[ct])), top - from);  // bits of the largest probability, or of a part of l
-                    const float by = first || most > kTopBits ? most - kLiftBits : 0.0f;  // too many
+                    const float peak = fmaxf(__log2f(max_groups(l[ct])) - gap, __builtin_fmaf(score, mult[ct], -from));  // of the probabilities, or of l's parts
+                    const float by = most + gap > kTopBits ? most - kLiftBits : -gap;  // that the reference should be above `from`; as it is, without need
                     float up = fminf(fmaxf(by, peak - 90.0f), peak + 60.0f);
-                    if (!(fabsf(from) < 0x1p20f)) up = fmaxf(top - from, 0.0f);  // so far off that references are no longer so near one another
-                    const bool none = peak == -INFINITY;
+                    if (none || !(fabsf(from) < 0x1p20f)) up = 0.0f;  // (so far off, references are not so near one another)
                     m[ct] = none ? -INFINITY : from + up;
-                    up = none ? 0.0f : m[ct] - from;
-                    const float rest = fabsf(up - by) > 1.0f ? fminf(apart[ct] + (up - by), 115.0f - fmaxf(peak - up, 0.0f)) : apart[ct];
-                    const float f = pow2(rest - apart[ct] - up);
+                    if (!none) up = m[ct] - from;
+                    const float rest = !none && fabsf(up - by) > 1.0f ? fminf(apart[ct] + (up - by), 115.0f - fmaxf(peak - up, 0.0f)) : apart[ct];
+                    const float f = pow2(rest - apart[ct] - up - gap);
                     each<DT>([&](auto dt) { o[ct][decltype(dt)::value] *= f; });
-                    l[ct] *= pow2(-up);
+                    l[ct] *= pow2(-up - gap);
                     apart[ct] = rest;
                     aparts = aparts || __any(rest != 0.0f);
                     pin(ct);

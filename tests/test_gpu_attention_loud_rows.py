@@ -67,10 +67,10 @@ def test_scales_at_the_ends_of_their_range(at, ref, n, format):
 @pytest.mark.parametrize("format", FORMATS)
 @pytest.mark.parametrize("n", DRAFTS)
 def test_scores_beyond_what_references_tell_apart(at, ref, n, format):
-    """Scores of 10^9, whose neighbours in fp32 are tens apart, with loud and quiet values: one key is all there is."""
+    """Scores of 10^8, whose neighbours in fp32 are tens apart, with loud and quiet values: one key is all there is."""
     g = gen_of(34, n)
     for k in (0, 20, -60, 90):
         K, V = rand(g, 200 + n, 1, 64, dtype="bf16"), rand(g, 200 + n, 1, 64, dtype="bf16")
         V[::2] *= 2.0 ** k
         p = Paged(at, ref, g, [200], [n], 4, 1, 64, "bf16", format, K=[K], V=[V])
-        check(at, ref, p, 64, None, scale=1e8)
+        check(at, ref, p, 64, None, scale=1e7)
