@@ -545,7 +545,8 @@ typedef struct {
     int64_t q_token, q_head, o_token, o_head; /* strides of Q and out; 0: heads*D and D           */
 } mmoe_attend_shape;
 
-/* Host only, pure.  Workspace (bytes), 0 if the shape is invalid. */
+/* Host only, pure.  Workspace (bytes) of mmoe_attend, never less for fewer requests, tokens, drafts or pages, whatever the hints of those calls
+ * (with a sum_keys here: for calls whose own, given or n_requests * max_keys, is up to that).  0 if the shape is invalid. */
 size_t mmoe_attend_workspace_bytes(const mmoe_attend_shape *shape);
 
 /* Q [T, heads, D], starts [n_requests + 1], ctx [n_requests], tree [T, mask_words] uint64 or NULL, pages [n_requests,

@@ -5,6 +5,7 @@
 namespace mmoe {
 
 constexpr int kMaxShares = 4096;
+constexpr int kMostShared = 1024;  // workgroups of a call whose pages are shared out: two rounds (of 27000 plans 38 would have more); bounds the workspace
 constexpr int kManyParts = 8;  // of a request on average: four wavefronts join them (us, 32 heads, attention with the join by one wavefront and by four:
                               // 1 request of 60000 keys 37, 31; 4 of 8000 28.2, 26.8; but 8 tokens of 32 requests 67, 76; 512 of 3 242, 299)
 
@@ -121,7 +122,7 @@ static double shares_for(const mmoe_attend_shape& s, int sets, bool three, Share
         // rounds of resident workgroups, or shares of a few pages
         const int64_t tries[] = {room / heads, 2 * room / heads, 3 * room / heads, 4 * room / heads, pages, pages / 2, pages / 4, pages / 8, pages / 16, pages / 32};
         for (int64_t w : tries) {
-            if (w < 2 || w > kMaxShares || w > pages) continue;
+            if (w < 2 || w > kMaxShares || w > pages || w * heads > kMostShared) continue;
             const double each = (double)pages / w, taken = 1.0 + (double)s.n_requests / w;  // pages, requests of a share
             const double active = fmin((double)w * heads, (double)room) / r.groups;
             const double one = fmax(page, bytes * active * 4.0 / r.sets / kRate);
@@ -166,10 +167,19 @@ bool attend_fits(const mmoe_attend_shape& s)
 static int64_t columns_of(const mmoe_attend_shape& s) { return (int64_t)(s.max_drafts < s.T ? s.max_drafts : s.T) * (s.heads / s.cache.kv_heads); }
 static size_t part_rows(const mmoe_attend_shape& s, const Shares& r) { return (size_t)r.shares * 2 * s.cache.kv_heads * columns_of(s); }
 
+static size_t parts_bytes(const mmoe_attend_shape& s, size_t rows) { return 256 + align256(rows * s.cache.head_dim * 4) + align256(rows * 8); }
+
+// What a call of this shape uses.
+size_t attend_need(const mmoe_attend_shape& s) { return parts_bytes(s, part_rows(s, shares_of(s))); }
+
+// The most that one of up to these requests, tokens, drafts, pages and keys does: fewer requests may have more shares.  A workgroup of a share has
+// 2 * 128 rows of parts at most, and a share is a page or more.
 size_t attend_ws_bytes(const mmoe_attend_shape& s)
 {
-    const size_t rows = part_rows(s, shares_of(s));
-    return 256 + align256(rows * s.cache.head_dim * 4) + align256(rows * 8);
+    const int64_t cap = (int64_t)s.max_pages * kPage, most = (int64_t)s.n_requests * cap, C = columns_of(s);
+    const int64_t pages = (s.sum_keys ? s.sum_keys : most) / kPage + s.n_requests;
+    const int64_t by_shares = 2 * kMostShared * (C < 128 ? C : 128), by_pages = 2 * (pages < kMaxShares ? pages : kMaxShares) * s.cache.kv_heads * C;
+    return parts_bytes(s, (size_t)(by_shares < by_pages ? by_shares : by_pages));
 }
 
 int launch_attend(const mmoe_attend_shape& s, const void* Q, const int32_t* starts, const int32_t* ctx, const uint64_t* tree,

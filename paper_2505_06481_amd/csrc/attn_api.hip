@@ -242,7 +242,7 @@ int mmoe_attend(const mmoe_attend_shape* shape, const void* Q, const int32_t* st
     if (!Q || !starts || !ctx || !pages || !out) return MMOE_ERR_NULL;
     if (tree && shape->mask_words <= 0) return MMOE_ERR_DIM;
     if (int rc = check_cache_pointers(shape->cache, cache)) return rc;
-    if (!ws || ws_bytes < attend_ws_bytes(*shape)) return MMOE_ERR_WORKSPACE;
+    if (!ws || ws_bytes < attend_need(*shape)) return MMOE_ERR_WORKSPACE;
     if (misaligned(Q, 16) || misaligned(out, 16) || misaligned(starts, 4) || misaligned(ctx, 4) || misaligned(pages, 4) ||
         misaligned(tree, 8) || misaligned(lse, 4) || misaligned(ws, 256))
         return MMOE_ERR_ALIGN;

@@ -75,6 +75,7 @@ int launch_cache_read(const mmoe_cache_shape& s, const mmoe_cache& cache, int R,
                       hipStream_t st);
 
 bool attend_fits(const mmoe_attend_shape& s);
+size_t attend_need(const mmoe_attend_shape& s);
 size_t attend_ws_bytes(const mmoe_attend_shape& s);
 int launch_attend(const mmoe_attend_shape& s, const void* Q, const int32_t* starts, const int32_t* ctx, const uint64_t* tree,
                   const int32_t* pages, const mmoe_cache& cache, void* out, float* lse, void* ws, hipStream_t st);
