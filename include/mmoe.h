@@ -538,6 +538,7 @@ typedef struct {
     int32_t heads;      /* query heads, a multiple of kv_heads, up to 64 to a key head            */
     int32_t max_pages;  /* columns of `pages`; positions from 64*max_pages on are not seen        */
     int32_t max_drafts; /* no request has more tokens in Q; what goes beyond is not written       */
+                        /* (MMOE_ERR_LIMIT where n_requests * heads * max_drafts needs 2^24 workgroups, 64 or 128 rows each) */
     int32_t mask_words; /* 64-bit words of a row of `tree`                                        */
     int32_t max_keys;   /* hint: the longest ctx + n; 0: 64*max_pages.  Results do not depend on the hints beyond rounding */
     int64_t sum_keys;   /* hint: the sum of ctx + n; 0: n_requests * max_keys                     */

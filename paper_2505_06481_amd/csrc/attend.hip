@@ -5,6 +5,7 @@
 namespace mmoe {
 
 constexpr int kMaxShares = 4096;
+constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;  // workgroups of 256: a launch has fewer than 2^32 threads
 constexpr int kMostShared = 1024;  // workgroups of a call whose pages are shared out: two rounds (of 27000 plans 38 would have more); bounds the workspace
 constexpr int kManyParts = 8;  // of a request on average: four wavefronts join them (us, 32 heads, attention with the join by one wavefront and by four:
                               // 1 request of 60000 keys 37, 31; 4 of 8000 28.2, 26.8; but 8 tokens of 32 requests 67, 76; 512 of 3 242, 299)
@@ -118,7 +119,8 @@ static double shares_for(const mmoe_attend_shape& s, int sets, bool three, Share
     const double even = fmax(work((double)pages * heads / room, page), (double)pages * s.cache.kv_heads * bytes / kRate);  // all of it, spread evenly
     double least = kRequest * ((s.n_requests * heads + room - 1) / room) + fmax(work((double)most_pages, page), even);
     r.shares = 0;
-    if (s.n_requests <= kMaxShared && s.n_requests * (int64_t)s.max_pages < (int64_t)1 << 30) {
+    const int64_t rows = C / G * s.heads;  // of a request: the join's grid
+    if (s.n_requests <= kMaxShared && s.n_requests * (int64_t)s.max_pages < (int64_t)1 << 30 && rows * s.n_requests <= kMostGroups) {
         // rounds of resident workgroups, or shares of a few pages
         const int64_t tries[] = {room / heads, 2 * room / heads, 3 * room / heads, 4 * room / heads, pages, pages / 2, pages / 4, pages / 8, pages / 16, pages / 32};
         for (int64_t w : tries) {
@@ -154,13 +156,11 @@ static Shares shares_of(const mmoe_attend_shape& s)
     return r;
 }
 
-// Whether the grids' sizes fit.
+// Whether the grid's size fits.
 bool attend_fits(const mmoe_attend_shape& s)
 {
     const Shares r = shares_of(s);
-    const int64_t drafts = s.max_drafts < s.T ? s.max_drafts : s.T, most = ((int64_t)1 << 31) - 1;
-    return drafts * s.heads < most && drafts * s.heads * s.n_requests <= most &&
-           ((int64_t)s.cache.kv_heads * (r.shares ? r.shares : s.n_requests) + 8) * r.groups <= most;
+    return ((int64_t)s.cache.kv_heads * (r.shares ? r.shares : s.n_requests) + 7) / 8 * 8 * r.groups <= kMostGroups;
 }
 
 // Columns of a request at most, and rows of partial results.

@@ -54,3 +54,14 @@ def test_workspace_is_never_less_for_smaller_calls(at, D, dtype, format):
             T = rng.randint(1, n2 * d2)
             part = at.make_attend_shape(cs, T, n2, kv * G, p2, d2, 1.0, max_keys=keys, sum_keys=total)
             assert need(at, part) <= most and (hint or at.attend_workspace_bytes(part) <= most)
+
+
+def test_grids_that_no_launch_has(at):
+    """A launch has fewer than 2^32 threads: calls beyond are refused by the host, and no plan has a join beyond."""
+    cs = at.make_cache_shape(1 << 20, 8, 128, "bf16", "int8")
+    for n, prompt in ((2048, 4096), (512, 65536), (1 << 16, 64)):
+        assert need(at, at.make_attend_shape(cs, n + prompt, n, 32, 2000, prompt, 1.0)) > 0
+        assert at.attend_workspace_bytes(at.make_attend_shape(cs, n + prompt, n, 32, 2000, prompt, 1.0)) > 0
+    one = at.make_cache_shape(1 << 20, 1, 128, "bf16", "int8")
+    assert at.attend_workspace_bytes(at.make_attend_shape(one, 1 << 20, 1, 64, 2000, 1 << 20, 1.0)) > 0
+    assert at.attend_workspace_bytes(at.make_attend_shape(one, 1 << 24, 1, 64, 2000, 1 << 24, 1.0)) == 0
