@@ -172,9 +172,11 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
             for (int e = 0; e < 4; ++e) lds.part[wave][i * 16 + lg * 4 + e][j * 16 + lr] = acc[i][j][e];
     __syncthreads();
     const float f = g.scale[a];
-    for (int i = tid; i < count * cols; i += 256) {  // cols: those of U from rb0 on; the padding's are zeros
+    // cols: those of U from rb0 on; the padding's are zeros (not the sums of padded A's zeros, which an infinite X makes NaN)
+    const int ranks = min(g.R - rb0 * 16, RB * 16);
+    for (int i = tid; i < count * cols; i += 256) {
         const int tok = i / cols, r = i % cols;
-        const float v = r < RB * 16 ? (lds.part[0][r][tok] + lds.part[1][r][tok] + (lds.part[2][r][tok] + lds.part[3][r][tok])) * f : 0.0f;
+        const float v = r < ranks ? (lds.part[0][r][tok] + lds.part[1][r][tok] + (lds.part[2][r][tok] + lds.part[3][r][tok])) * f : 0.0f;
         const int64_t to = (int64_t)lds.tokens.list[at + tok] * g.Rp * kParts + rb0 * 16 + r;
         if (F32) {
             ((float*)g.U)[to] = v;
