@@ -47,8 +47,9 @@ int launch_pack_pieces(const void* in, void* out, int S, int K, int N, int Kp, i
 }
 
 // ---- U = scale (X A) ----------------------------------------------------------------------------------
-// With bf16 storage U is kept as two bf16 parts, the value rounded and what that leaves, [T][2][Rp]: the second product runs
-// on the bf16 instruction with 16 bits of U, so the adapter adds no error of its own to the rounding of Y.
+// With bf16 storage U is kept as two bf16 parts, its first 8 bits and what they leave, [T][2][Rp]: the second product runs
+// on the bf16 instruction with 16 bits of U, so the adapter adds no error of its own to the rounding of Y.  Both parts have the sign of U and neither
+// is zero or infinite where U is not (down to 2^-110), so that an infinity in B gives one of its sign, not NaN.
 //
 // A workgroup takes the tokens of one adapter among a chunk of the batch, 32 at a time; its four wavefronts a quarter of K each.
 // (32 tokens fill two columns' tiles: fewer read the adapter more often, more leave compute units idle.  8192 tokens of 4096, 2 adapters: 26 us,
@@ -125,6 +126,17 @@ __device__ __forceinline__ int adapter_of(const int32_t* aid, int t0, int count,
     return __all(first) ? a : -1;
 }
 
+// v = hi + lo, 2^-16 of v apart at most; hi is cut, not rounded: rounded, it would be infinite above bf16's largest number.
+__device__ __forceinline__ void split_bf16(float v, uint16_t& hi, uint16_t& lo)
+{
+    const uint32_t bits = __float_as_uint(v);
+    hi = (uint16_t)(bits >> 16);
+    const float left = v - bf16_bits_to_f32(hi);
+    lo = f32_to_bf16_bits(left);
+    if (left == 0.0f && fabsf(v) >= 0x1p-110f) lo = (uint16_t)((hi & 0x8000) | 0x0080);  // 2^-126
+    if (!(fabsf(v) < INFINITY)) lo = fabsf(v) == INFINITY ? hi : (uint16_t)0;            // NaN: the first part's
+}
+
 template <bool F32, int RB>
 __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds, int a, int rb0, int cols, int at, int count)
 {
@@ -181,10 +193,10 @@ __device__ __forceinline__ void shrink_tiles(const ShrinkArgs& g, ShrinkLds& lds
         if (F32) {
             ((float*)g.U)[to] = v;
         } else {
-            const uint16_t hi = f32_to_bf16_bits(v);
+            uint16_t hi, lo;
+            split_bf16(v, hi, lo);
             ((uint16_t*)g.U)[to] = hi;
-            const float left = v - bf16_bits_to_f32(hi);  // NaN where v is not finite: then the rounded value is all
-            ((uint16_t*)g.U)[to + g.Rp] = f32_to_bf16_bits(left == left ? left : 0.0f);
+            ((uint16_t*)g.U)[to + g.Rp] = lo;
         }
     }
 }
