@@ -420,8 +420,8 @@ int mmoe_project(const mmoe_project_shape *shape, const void *X, const int32_t *
  * x[2i+1]) (MMOE_ROTARY_NEIGHBOURS) and turns by the angle pos[t] f_i:
  *   y0 = m (x0 cos - x1 sin),  y1 = m (x0 sin + x1 cos);   with `transpose` the sine's sign is swapped: the
  *   transposed map, which takes a gradient of y to the gradient of x.
- * Elements from rot on are copied.  Angles are kept in units of 2^-64 turn, where whole turns overflow: they are
- * exact to 2^-32 turn at every position.
+ * Elements from rot on are copied.  Angles are kept in units of 2^-64 turn, where whole turns overflow, and rounded to fp32 as
+ * fractions of a turn: within 2^-26 turn (that rounding) and |pos| 2^-55 (f_i is a double) of pos f_i at every position.
  *
  * f_i = base^(-2i/rot), changed for contexts longer than `original`, the one trained for, by `factor`:
  *   LINEAR  f_i / factor
@@ -528,8 +528,9 @@ int mmoe_cache_read(const mmoe_cache_shape *shape, const mmoe_cache *cache, int3
  *   out[t,h] = sum_j softmax_j(scale <Q[t,h], K[j]>) V[j];  lse[t,h] = ln sum_j exp(scale <Q[t,h], K[j]>)
  * A token that sees nothing gets zeros and an lse of -infinity.  What a token does not see does not reach it, whatever it
  * holds: rows of a page past the end, infinities, NaN.  Scores, maxima, sums and outputs are fp32.  The probabilities are
- * rounded for the second product: to bf16 over PLAIN bf16 pages, to fp16 over 8-bit ones, whose codes fp16 holds exactly
- * (and queries there to fp16, relative to the row's largest; with fp32 nothing is rounded).  8-bit formats need dtype bf16 here.
+ * rounded for the second product: to bf16 over PLAIN bf16 pages; with their value's scale to fp16 over 8-bit ones, 11 bits down to 2^-30 of
+ * the token's largest, whose codes fp16 holds exactly (and queries there to fp16, relative to the row's largest; with fp32 nothing is
+ * rounded).  The fp32 sums have room for scores of up to 2^28 and values of up to 2^100.  8-bit formats need dtype bf16 here.
  */
 typedef struct {
     mmoe_cache_shape cache;

@@ -47,7 +47,8 @@ __device__ __forceinline__ UnitPlace unit_place(int u, int rot)
     return {16 * u, 16 * u + 8};
 }
 
-// (The angle's error is 2^-25 turn, the rounding to fp32, at any position: a product in fp32 would be off by whole turns from 2^24 on.)
+// (The angle's error is 2^-26 turn, the rounding to fp32, at any position, and 2^-55 of a turn for each position, the steps': a product in fp32 would
+// be off by whole turns from 2^24 on.)
 // Cosine and sine of pairs 8u .. 8u+7 at a position, times m.  steps: turns per position in units of 2^-64; the product's
 // overflow is whole turns.  The upper 32 bits, as a signed number, are the angle in [-1/2, 1/2) turn.
 __device__ __forceinline__ void turn_of(const uint64_t* __restrict__ steps, int pos, float m, float sign, float* c, float* s)
