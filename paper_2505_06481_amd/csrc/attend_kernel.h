@@ -526,11 +526,11 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
                 sum += s[ct][kt][e];
             });
             if constexpr (kCodes) {
+                each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= vs[decltype(kt)::value]; });
                 if (aparts) {
                     const float f = pow2(apart[ct]);
                     each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= f; });
                 }
-                each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= vs[decltype(kt)::value]; });
                 if (tail)  // 0 times a scale that is not a number
                     each<KT * 4>([&](auto x) {
                         constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
