@@ -488,9 +488,7 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
                 // (never where top is -infinity; not top - m: far off, its rounding is many bits that the exponents do not have)
                 if (__any(__builtin_fmaf(score, mult[ct], -m[ct]) > fminf(room - apart[ct], kMostBits))) {
                     each<KT>([&](auto kt) { only_here(s[ct][decltype(kt)::value]), only_here(vs[decltype(kt)::value]); });
-                    const float high = fmaxf(m[ct], top);
-                    const bool none = high == -INFINITY;
-                    const float from = none ? 0.0f : high, gap = from - m[ct];  // (infinite where there was nothing so far)
+                    const float from = fmaxf(m[ct], top), gap = from - m[ct];  // (infinite where there was nothing so far, NaN where there still is not)
                     float most = -INFINITY;  // log2 of the largest product that the column sees: a scale's bits are 2^23 (log2 + 127) less 0 to 0.09
                     each<KT * 4>([&](auto x) {
                         constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
@@ -498,15 +496,16 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
                     });
                     most = max_groups(most) - 126.9f + apart[ct];
                     const float peak = fmaxf(__log2f(max_groups(l[ct])) - gap, __builtin_fmaf(score, mult[ct], -from));  // of the probabilities, or of l's parts
-                    const float by = most + gap > kTopBits ? most - kLiftBits : -gap;  // that the reference should be above `from`; as it is, without need
+                    const bool stay = !(most + gap > kTopBits || peak + gap > 90.0f);  // a row was in doubt that the column sees with a small product, or not
+                    const float by = most + gap > kTopBits ? most - kLiftBits : -gap;  // that the reference should be above `from`
                     float up = fminf(fmaxf(by, peak - 90.0f), peak + 60.0f);
-                    if (none || !(fabsf(from) < 0x1p20f)) up = 0.0f;  // (so far off, references are not so near one another)
-                    m[ct] = none ? -INFINITY : from + up;
-                    if (!none) up = m[ct] - from;
-                    const float rest = !none && fabsf(up - by) > 1.0f ? fminf(apart[ct] + (up - by), 115.0f - fmaxf(peak - up, 0.0f)) : apart[ct];
-                    const float f = pow2(rest - apart[ct] - up - gap);
+                    if (!(fabsf(from) < 0x1p20f)) up = 0.0f;  // (so far off, references are not so near one another)
+                    m[ct] = stay ? m[ct] : from + up;
+                    up = m[ct] - from;
+                    const float rest = !stay && fabsf(up - by) > 1.0f ? fminf(apart[ct] + (up - by), 115.0f - fmaxf(peak - up, 0.0f)) : apart[ct];
+                    const float f = stay ? 1.0f : pow2(rest - apart[ct] - up - gap);
                     each<DT>([&](auto dt) { o[ct][decltype(dt)::value] *= f; });
-                    l[ct] *= pow2(-up - gap);
+                    l[ct] *= stay ? 1.0f : pow2(-up - gap);
                     apart[ct] = rest;
                     aparts = aparts || __any(rest != 0.0f);
                     pin(ct);

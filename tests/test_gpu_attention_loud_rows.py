@@ -74,3 +74,20 @@ def test_scores_beyond_what_references_tell_apart(at, ref, n, format):
         V[::2] *= 2.0 ** k
         p = Paged(at, ref, g, [200], [n], 4, 1, 64, "bf16", format, K=[K], V=[V])
         check(at, ref, p, 64, None, scale=1e7)
+
+
+@pytest.mark.parametrize("format", FORMATS)
+@pytest.mark.parametrize("n", [1, 12, 16])
+def test_loud_rows_in_every_step(at, ref, n, format):
+    """A loud row of small probability on every page of a long context: the reference is looked at again and again, and stays what it is."""
+    g = gen_of(35, n)
+    ctx, D = 6000, 64
+    K, V = rand(g, ctx + n, 1, D, dtype="bf16"), rand(g, ctx + n, 1, D, dtype="bf16")
+    K[..., 0] = 4.0
+    K[7:ctx:50, :, 0] = 4.0 - 60 / 8.0
+    V[7:ctx:50] *= 2.0 ** 40
+    p = Paged(at, ref, g, [ctx], [n], 4, 1, D, "bf16", format, K=[K], V=[V])
+    p.Q *= 0.25
+    p.Q[..., 0] = 8.0
+    check(at, ref, p, D, None, scale=1.0)
+    check(at, ref, p, D, None, scale=1.0, max_keys=ctx + n, sum_keys=ctx + n)
