@@ -526,15 +526,15 @@ __global__ __launch_bounds__(256, (attend_waves<D, KIND, NC>())) void attend_ker
             });
             if constexpr (kCodes) {
                 each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= vs[decltype(kt)::value]; });
-                if (aparts) {
+                if (tail || aparts) {
                     const float f = pow2(apart[ct]);
-                    each<KT>([&](auto kt) { s[ct][decltype(kt)::value] *= f; });
-                }
-                if (tail)  // 0 times a scale that is not a number
-                    each<KT * 4>([&](auto x) {
+                    uint64_t seen = vis[ct];
+                    only_here(seen);
+                    each<KT * 4>([&](auto x) {  // (0 times a scale may be NaN)
                         constexpr int kt = decltype(x)::value / 4, e = decltype(x)::value % 4;
-                        if (!(vis[ct] & (uint64_t)1 << (kt * 16 + e))) s[ct][kt][e] = 0.0f;
+                        s[ct][kt][e] = seen & (uint64_t)1 << (kt * 16 + e) ? s[ct][kt][e] * f : 0.0f;
                     });
+                }
             }
             l[ct] += sum;
             // tiles to operand pieces: 16-bit ones hold two tiles' keys
