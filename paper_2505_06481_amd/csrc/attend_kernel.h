@@ -12,8 +12,8 @@
 // instruction, no LDS and no barrier in the loop.  Queries of more than 16 columns stand in LDS in operand order.
 //
 // Bound by the cache's bytes up to 32 columns (8 requests of 60000 fp8 keys, 32 heads on 8 of 128: single tokens 185 us, 5.5 TB/s; 8 tokens
-// each 199 us, 5.1 TB/s), then more and more by vector instructions (16 tokens, 64 columns: 4.8 TB/s), fp32 by its matrix rate, few keys by
-// latency (4 requests of up to 700: 9.7 us).  8-bit codes widen to fp16, which holds them exactly; their key scales multiply scores and
+// each 199 us, 5.1 TB/s), then more and more by vector instructions (16 tokens, 64 columns: 4.6 TB/s), fp32 by its matrix rate, few keys by
+// latency (4 requests of up to 700: 9.8 us).  8-bit codes widen to fp16, which holds them exactly; their key scales multiply scores and
 // their value scales probabilities, so pages are never written out in 16 bits.
 //
 // Roundings below 32 bits: probabilities to bf16 or, with their value's scale, fp16, the operand type of the second product (8 and
