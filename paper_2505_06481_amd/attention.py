@@ -307,6 +307,7 @@ def attend_workspace_bytes(shape: AttendShape) -> int:
 
 
 def attend_workspace(shape: AttendShape, device="cuda") -> torch.Tensor:
+    """For calls of this shape and of fewer requests, tokens, drafts or pages (with ``sum_keys`` set: of up to as many keys)."""
     n = attend_workspace_bytes(shape)
     if n == 0:
         raise ValueError("mmoe_attend_workspace_bytes: the shape is not valid")
